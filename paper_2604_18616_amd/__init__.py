@@ -5,11 +5,13 @@ library built from ``csrc/``; every step of the computation runs in the HIP kern
 :mod:`.inputs` generates the seeded synthetic workloads.
 """
 
-__all__ = ["attn_fwd", "gemm_bf16", "moe_ffn_fp8", "load_library", "build_library", "inputs"]
+__all__ = ["attn_fwd", "gemm_bf16", "moe_ffn_fp8", "rope_bf16", "rope_frequencies", "KvFp8Cache", "kv_fp8_cache", "kv_fp8_write", "kv_fp8_read", "attn_kv_fp8",
+           "load_library", "build_library", "inputs"]
 
 
 def __getattr__(name):
-    if name in ("attn_fwd", "gemm_bf16", "moe_ffn_fp8", "moe_workspace_bytes", "load_library", "attn_fwd_flops", "strerror", "version", "AttnError"):
+    if name in ("attn_fwd", "gemm_bf16", "moe_ffn_fp8", "moe_workspace_bytes", "load_library", "attn_fwd_flops", "rope_bf16", "rope_frequencies",
+                "KvFp8Cache", "kv_fp8_cache", "kv_fp8_write", "kv_fp8_read", "attn_kv_fp8", "strerror", "version", "AttnError"):
         from . import binding
         return getattr(binding, name)
     if name == "build_library":

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import Any, NamedTuple
 
 from .build import LIB_PATH, NATIVE_PATH, build_library, stale_sources
 
@@ -70,6 +71,18 @@ def load_library(build_if_missing: bool = True):
         lib.moe_ffn_fp8_static.argtypes = [p, p, p, p, p, p, p, p, i, i, i, i, i, p]
         lib.moe_ffn_fp8_flops_per_pair.restype = ctypes.c_double
         lib.moe_ffn_fp8_flops_per_pair.argtypes = [i, i]
+        lib.kv_fp8_write.restype = i
+        lib.kv_fp8_write.argtypes = [p, p, p, p, p, p, ll, i, p, p, i, i, p]
+        lib.kv_fp8_read.restype = i
+        lib.kv_fp8_read.argtypes = [p, p, ll, i, p, p, p, p, p, i, i, i, p]
+        lib.attn_kv_fp8_workspace_bytes.restype = ctypes.c_size_t
+        lib.attn_kv_fp8_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
+        lib.attn_kv_fp8.restype = i
+        lib.attn_kv_fp8.argtypes = [p, p, p, ll, i, p, p, p, p, i, i, i, p, p, i, i, i, f, i, p, ctypes.c_size_t, i, p]
+        lib.rope_bf16.restype = i
+        lib.rope_bf16.argtypes = [p, p, p, p, i, i, i, i, i, i, p, p, p, p, p, ll, p, i, i, f, p]
+        lib.rope_frequencies.restype = i
+        lib.rope_frequencies.argtypes = [i, ctypes.c_double, ctypes.c_double, i, ctypes.c_double, ctypes.c_double, p]
         lib.attn_strerror.restype = ctypes.c_char_p
         lib.attn_strerror.argtypes = [i]
         lib.attn_version.restype = i
@@ -357,3 +370,192 @@ def moe_ffn_fp8(x, ids, wts, w13, s13, w2, s2, y=None, workspace=None, stream=No
     if rc != 0:
         raise AttnError(rc, strerror(rc))
     return y
+
+
+class KvFp8Cache(NamedTuple):
+    """The tensors of a quantised cache (include/kv_cache.h): codes as uint8, k [pages, Hkv, page, D] and v [pages, Hkv, D, page];
+    exponents + 127 as uint8 [pages, Hkv].  All contiguous, on one CUDA device; kv_fp8_cache makes one."""
+    k: Any
+    v: Any
+    k_exp: Any
+    v_exp: Any
+
+
+class _CacheStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("pages", ctypes.c_int), ("Hkv", ctypes.c_int), ("page", ctypes.c_int), ("D", ctypes.c_int)]
+
+
+def kv_fp8_cache(pages, Hkv, page, D, device="cuda") -> KvFp8Cache:
+    """An empty cache of `pages` pages of `page` tokens (16, 32, 64 or 128) for Hkv kv heads of dimension D (64 or 128); its
+    contents mean nothing before they are written."""
+    import torch
+    codes = lambda *shape: torch.empty(shape, dtype=torch.uint8, device=device)
+    return KvFp8Cache(codes(pages, Hkv, page, D), codes(pages, Hkv, D, page), codes(pages, Hkv), codes(pages, Hkv))
+
+
+def _cache_struct(cache):
+    """The C structure of a cache, checked; its head count and dimension, its device."""
+    import torch
+    k, v, ke, ve = cache
+    for t in cache:
+        if not t.is_cuda:
+            raise ValueError("the cache must be CUDA tensors: there is no CPU path")
+        if t.dtype != torch.uint8 or not t.is_contiguous():
+            raise ValueError("the cache must be contiguous uint8 tensors")
+    if k.dim() != 4:
+        raise ValueError("k codes must be [pages, Hkv, page, D]")
+    P, H, page, D = k.shape
+    if v.shape != (P, H, D, page) or ke.shape != (P, H) or ve.shape != (P, H):
+        raise ValueError("inconsistent cache shapes: k [pages, Hkv, page, D], v [pages, Hkv, D, page], k_exp and v_exp [pages, Hkv]")
+    if v.device != k.device or ke.device != k.device or ve.device != k.device:
+        raise ValueError("the cache must live on one CUDA device")
+    return _CacheStruct(k.data_ptr(), v.data_ptr(), ke.data_ptr(), ve.data_ptr(), P, H, page, D), H, D, k.device
+
+
+def _table(table, device):
+    """(address, pitch, batch, width) of a page table."""
+    import torch
+    if table.dtype != torch.int32 or table.dim() != 2 or table.device != device or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("the page table must be int32 [B, width] with contiguous rows on the cache's device")
+    return table.data_ptr(), table.stride(0), table.shape[0], table.shape[1]
+
+
+def _per_sequence(t, B, device, name):
+    """Address of an int32 [B] tensor, None for None."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != (B,) or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 tensor of shape [B] on the cache's device" % name)
+    return t.data_ptr()
+
+
+def _rows(t, shape, device, name):
+    """Strides of a bf16 [B, heads, S, D] tensor with contiguous rows."""
+    import torch
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != tuple(shape) or t.device != device or t.stride(3) != 1:
+        raise ValueError("%s must be bfloat16 %s with contiguous rows on one CUDA device" % (name, list(shape)))
+    return _strides3(t)
+
+
+def kv_fp8_write(cache, k, v, table, start, count=None, stream=None):
+    """Append k, v (bf16 [B, Hkv, S, D], strided views as in attn_fwd) to a quantised cache: token t of sequence b, t < count[b]
+    (all where count is None), goes to position start[b] + t, which lies on page table[b][position // page].  table int32
+    [B, width], start and count int32 [B], all on the GPU.  Enqueued on `stream` (default: torch's current stream); no sync.
+    Returns the cache."""
+    struct, H, D, device = _cache_struct(cache)
+    at, pitch, B, width = _table(table, device)
+    if k.dim() != 4:
+        raise ValueError("k and v must be [B, Hkv, S, D]")
+    S = k.shape[2]
+    ks, vs = (_rows(t, (B, H, S, D), device, name) for t, name in ((k, "k"), (v, "v")))
+    stream, _ = _streams(k, stream)
+    rc = load_library().kv_fp8_write(ctypes.byref(struct), k.data_ptr(), v.data_ptr(), ks, vs, at, pitch, width,
+                                     _per_sequence(start, B, device, "start"), _per_sequence(count, B, device, "count"), B, S, stream)
+    if rc != 0:
+        raise AttnError(rc, strerror(rc))
+    return cache
+
+
+def kv_fp8_read(cache, table, lens, S, first=0, k=None, v=None, stream=None):
+    """k, v (bf16 [B, Hkv, S, D]) of positions first ... first + S - 1 of every sequence, zeros at positions from lens[b] on and
+    on missing pages.  k and v are allocated with torch if not given.  Enqueued on `stream` (default: torch's current stream); no sync."""
+    import torch
+    struct, H, D, device = _cache_struct(cache)
+    at, pitch, B, width = _table(table, device)
+    shape = (B, H, int(S), D)
+    k = torch.empty(shape, dtype=torch.bfloat16, device=device) if k is None else k
+    v = torch.empty(shape, dtype=torch.bfloat16, device=device) if v is None else v
+    ks, vs = (_rows(t, shape, device, name) for t, name in ((k, "k"), (v, "v")))
+    stream, _ = _streams(k, stream)
+    rc = load_library().kv_fp8_read(ctypes.byref(struct), at, pitch, width, _per_sequence(lens, B, device, "lens"),
+                                    k.data_ptr(), v.data_ptr(), ks, vs, B, int(S), int(first), stream)
+    if rc != 0:
+        raise AttnError(rc, strerror(rc))
+    return k, v
+
+
+def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=False, window=0, sinks=0, scale=None, max_len=0, stream=None):
+    """O, LSE = attention of bf16 q [B, Hq, Sq, D] over a quantised cache: sequence b's lens[b] keys and values, of which the
+    q_lens[b] (all Sq where None) query rows are the last.  causal: row i sees the keys up to its own position; window > 0: of
+    those only the last `window` and the sequence's `sinks` first.  Rows that see nothing and rows from q_lens[b] on get O = 0
+    and LSE = -inf.  lens, q_lens int32 [B] on the GPU; max_len: no sequence is longer (0: the table's width).
+    o and lse as in attn_fwd.  Enqueued on `stream` (default: torch's current stream); no sync."""
+    import torch
+    struct, H, D, device = _cache_struct(cache)
+    at, pitch, B, width = _table(table, device)
+    if q.dim() != 4 or q.shape[1] % H:
+        raise ValueError("q must be [B, Hq, Sq, D] with Hq a multiple of the cache's heads")
+    Hq, Sq = q.shape[1], q.shape[2]
+    shape = (B, Hq, Sq, D)
+    qs = _rows(q, shape, device, "q")
+    o = torch.empty_like(q) if o is None else o
+    os_ = _rows(o, shape, device, "o")
+    if lse is None:
+        lse = torch.empty((B, Hq, Sq), dtype=torch.float32, device=device)
+    elif lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, Sq) or not lse.is_contiguous() or lse.device != device:
+        raise ValueError("lse must be a contiguous float32 tensor of shape [B, Hq, Sq] on q's device")
+    scale = float(D) ** -0.5 if scale is None else float(scale)
+    window, sinks, max_len = int(window), int(sinks), int(max_len)
+    lens, q_lens = _per_sequence(lens, B, device, "lens"), _per_sequence(q_lens, B, device, "q_lens")
+    stream, own = _streams(q, stream)
+    lib = load_library()
+    # memory for the parts of a cut call, only on the stream torch will reuse that memory on; elsewhere the call is not cut
+    most = width * struct.page
+    need = lib.attn_kv_fp8_workspace_bytes(B, Hq, H, Sq, min(max_len, most) if max_len > 0 else most, D, window, sinks) if own else 0
+    ws = _scratch(need, device) if need else None
+    rc = lib.attn_kv_fp8(q.data_ptr(), ctypes.byref(struct), at, pitch, width, lens, q_lens, o.data_ptr(), lse.data_ptr(), B, Hq, Sq, qs, os_,
+                         1 if causal else 0, window, sinks, scale, max_len, None if ws is None else ws.data_ptr(), need if ws is not None else 0, 0, stream)
+    if rc != 0:
+        raise AttnError(rc, strerror(rc))
+    return o, lse
+
+
+def rope_frequencies(R, base=10000.0, factor=1.0, original_len=0, slow=1.0, fast=32.0, device="cuda"):
+    """The frequencies of R rotated columns (float64 [R/2], radians per position) as rope_bf16 takes them; factor and
+    original_len stretch them for long contexts (include/rope.h)."""
+    import torch
+    if int(R) < 2 or int(R) % 2:
+        raise ValueError("R must be even and at least 2")
+    values = (ctypes.c_double * (int(R) // 2))()
+    rc = load_library().rope_frequencies(int(R), float(base), float(factor), int(original_len), float(slow), float(fast), values)
+    if rc != 0:
+        raise AttnError(rc, strerror(rc))
+    return torch.tensor(list(values), dtype=torch.float64, device=device)
+
+
+def rope_bf16(q, positions, inv_freq, k=None, q_out=None, k_out=None, interleaved=False, inverse=False, scale=1.0, stream=None):
+    """Rotary positions of bf16 q [B, Hq, S, D] and, in the same launch, k [B, Hk, S, D]: pair f of the 2 * len(inv_freq) first
+    columns turns by positions * inv_freq[f], times scale.  positions int32 [B, S] or [S]; inv_freq float64, both on the GPU.
+    interleaved: pairs are neighbouring columns, else the halves of the rotated part; inverse: the opposite angle (the
+    gradient).  Outputs are allocated with torch if not given and may be the inputs.  Returns q_out, or (q_out, k_out) with k.
+    Enqueued on `stream` (default: torch's current stream); no sync."""
+    import torch
+    if not q.is_cuda:
+        raise ValueError("q must be a CUDA tensor: there is no CPU path")
+    if q.dim() != 4:
+        raise ValueError("q must be [B, Hq, S, D]")
+    device, (B, Hq, S, D) = q.device, q.shape
+    qs = _rows(q, q.shape, device, "q")
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    qos = _rows(q_out, q.shape, device, "q_out")
+    Hk, ks, kos = 0, None, None
+    if k is not None:
+        Hk = k.shape[1] if k.dim() == 4 else 0
+        ks = _rows(k, (B, Hk, S, D), device, "k")
+        k_out = torch.empty_like(k) if k_out is None else k_out
+        kos = _rows(k_out, (B, Hk, S, D), device, "k_out")
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    if positions.dtype != torch.int32 or tuple(positions.shape) not in ((B, S), (S,)) or positions.device != device or (S > 1 and positions.stride(-1) != 1):
+        raise ValueError("positions must be int32 [B, S] or [S] with contiguous rows on q's device")
+    if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.device != device:
+        raise ValueError("inv_freq must be a contiguous float64 vector on q's device")
+    stream, _ = _streams(q, stream)
+    rc = load_library().rope_bf16(q.data_ptr(), q_out.data_ptr(), k.data_ptr() if Hk else None, k_out.data_ptr() if Hk else None, B, Hq, Hk, S, D,
+                                  2 * inv_freq.numel(), qs, qos, ks, kos, positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0,
+                                  inv_freq.data_ptr(), 1 if interleaved else 0, 1 if inverse else 0, float(scale), stream)
+    if rc != 0:
+        raise AttnError(rc, strerror(rc))
+    return q_out if k is None else (q_out, k_out)

@@ -15,7 +15,8 @@ LIB_PATH = os.path.join(_HERE, "libattn_mi355x.so")
 NATIVE_SRC = "native_calls.cpp"                      # the Python binding's plain calls, against torch's C++ interface
 NATIVE_PATH = os.path.join(_HERE, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))     # (for this Python only)
 SOURCES = ["attn_api.cpp", "attn_fwd_kernel.hip", "attn_split_kernel.hip", "gemm_api.cpp", "gemm_bf16_kernel.hip",
-           "gemm_unaligned_kernel.hip", "moe_api.cpp", "moe_fp8_kernel.hip"]
+           "gemm_unaligned_kernel.hip", "moe_api.cpp", "moe_fp8_kernel.hip", "kv_api.cpp", "kv_cache_kernel.hip", "attn_kv_kernel.hip",
+           "rope_api.cpp", "rope_kernel.hip"]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed-fp32 instructions are kept out of all device code: some of their forms have given wrong results on this hardware

@@ -1,0 +1,382 @@
+// Attention over the quantised paged cache, gfx950.
+//
+// The query rows that share a kv head (g = Hq / Hkv heads x Sq positions, the g heads of a position side by side) are packed
+// into blocks of 16, the columns of v_mfma_f32_16x16x32_bf16: S^T = K Q^T, O^T += V^T P^T, so that a row's running maximum
+// and sum are scalars of a lane.  A wavefront walks tiles of 64 keys on its own, straight from memory into registers, without
+// LDS and without barriers:
+//   * K: a lane reads 16 consecutive codes of its key, two steps of the matrix instruction (the order of the sum over d is
+//     free as long as Q is read in the same one);
+//   * row m of key block t of a tile stands for key 16 (m / 4) + 4 t + m % 4, so that after four blocks lane group l / 16
+//     holds the scores of 16 consecutive keys: the same 16 keys whose codes of one d are one 16-byte load of the transposed V;
+//   * codes become bf16, exactly and times the page's scale, by the conversion instruction; 16 keys lie in one page, so the
+//     scale and the page's address are per lane.
+// The keys are cut over the wavefronts of a workgroup and over `splits` workgroups; the wavefronts are merged through LDS,
+// the workgroups of a row by attn_kv_combine from fp32 parts.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "gfx950_prims.h"
+#include "kv_launch.h"
+
+namespace {
+
+using namespace gfx950;
+
+constexpr int kTile = 64;            // keys per tile
+constexpr int kWaves = 4;
+constexpr int kBlock = 16;           // packed query rows per block
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What the rows of a workgroup see of a sequence: tiles 0 ... sink_tiles - 1 and first ... first + count - sink_tiles - 1.
+struct Seen { int n, rows, pos0, count, sink_tiles, first; };
+__device__ __forceinline__ Seen seen_tiles(const KvAttnParams& p, int b, int g, int first_row, int rows_per_wg) {
+    Seen s;
+    s.n = min(max(p.lens[b], 0), p.max_len);
+    s.rows = p.q_lens ? min(max(p.q_lens[b], 0), p.Sq) : p.Sq;
+    s.pos0 = s.n - s.rows;                                   // position of query row 0
+    const int i0 = first_row / g, i1 = min((first_row + rows_per_wg - 1) / g, s.rows - 1);
+    s.count = s.sink_tiles = s.first = 0;
+    if (i0 > i1 || s.n == 0) return s;
+    const int last = p.causal ? min(s.n - 1, s.pos0 + i1) : s.n - 1;
+    if (last < 0) return s;
+    const long long low = p.window ? (long long)s.pos0 + i0 - p.window + 1 : 0;
+    s.first = low > 0 ? (int)(low / kTile) : 0;
+    s.sink_tiles = min(s.first, (int)(((long long)min(p.sinks, last + 1) + kTile - 1) / kTile));
+    s.count = s.sink_tiles + max(last / kTile + 1 - s.first, 0);
+    return s;
+}
+
+// The largest or the sum over the four lane groups that share a column.
+__device__ __forceinline__ float max_over_groups(float x) { x = fmaxf(x, __shfl_xor(x, 16)); return fmaxf(x, __shfl_xor(x, 32)); }
+__device__ __forceinline__ float sum_over_groups(float x) { x += __shfl_xor(x, 16); return x + __shfl_xor(x, 32); }
+
+// Eight codes (two dwords) as a matrix operand, times 2^e (scale: 2^e as fp32).
+__device__ __forceinline__ bf16x8 decode(unsigned lo, unsigned hi, float scale) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// The bytes of w that are the NaN code, as 0x80 each.
+__device__ __forceinline__ unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+template <int D> constexpr int merge_pitch() { return D + 4; }      // floats per O row in the merge area
+
+// NR blocks of 16 packed rows per workgroup, every wavefront all of them.
+template <int D, int NR>
+__global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
+    constexpr int KC = D / 64;                 // 16-byte loads per key and lane
+    constexpr int DT = D / 16;                 // 16-row blocks of O^T
+    constexpr int PITCH = merge_pitch<D>();
+    constexpr int ROWS = NR * kBlock;
+
+    __shared__ __attribute__((aligned(16))) float s_o[kWaves * ROWS * PITCH];
+    __shared__ float s_ml[2][kWaves][ROWS];
+    __shared__ float s_inv[ROWS];
+
+    const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, grp = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // Workgroup id -> (kv head of a sequence, split, row block); every XCD takes a contiguous range, so that row blocks of one
+    // split, which read the same keys, share an L2.
+    const int nb = gridDim.x, per_xcd = nb >> 3, bid = blockIdx.x;
+    int logical = bid < per_xcd * 8 ? (bid & 7) * per_xcd + (bid >> 3) : bid;
+    const int rowblk = logical % p.row_wgs; logical /= p.row_wgs;
+    const int split = logical % p.splits; logical /= p.splits;
+    const int hk = logical % p.c.Hkv, b = logical / p.c.Hkv;
+
+    const int g = p.Hq / p.c.Hkv, R = g * p.Sq, first = rowblk * ROWS;
+    const Seen seen = seen_tiles(p, b, g, first, ROWS);
+    const int per = (seen.count + p.splits - 1) / p.splits;
+    const int t0 = split * per, t1 = min(seen.count, t0 + per);
+    if (p.splits > 1 && t0 >= t1) return;                    // attn_kv_combine knows
+
+    // this lane's rows: what they see, and Q.  Rows past the last one see what the last one does and are not stored.
+    int hi[NR], lo[NR];
+    bf16x8 qf[NR][KC * 2];
+    int hi_all = -1, lo_all = INT_MAX;                       // what any row of the workgroup sees
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const int row = min(first + r * kBlock + col, R - 1), i = min(row / g, max(seen.rows - 1, 0)), h = row - row / g * g;
+        const int pos = seen.pos0 + i;
+        hi[r] = p.causal ? min(pos, seen.n - 1) : seen.n - 1;
+        lo[r] = p.window ? (int)max((long long)pos - p.window + 1, 0LL) : 0;
+        hi_all = max(hi_all, hi[r]); lo_all = min(lo_all, lo[r]);
+        const __bf16* const q = p.q + b * p.q_sb + (hk * g + h) * p.q_sh + (long long)i * p.q_ss;
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) qf[r][2 * c + u] = *(const bf16x8*)(q + (grp + 4 * c) * 16 + 8 * u);
+    }
+#pragma unroll
+    for (int x = 1; x < 16; x <<= 1) { hi_all = max(hi_all, __shfl_xor(hi_all, x)); lo_all = min(lo_all, __shfl_xor(lo_all, x)); }
+
+    f32x4 oacc[NR][DT];
+    float m_run[NR], l_run[NR];
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        m_run[r] = -INFINITY; l_run[r] = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) oacc[r][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float c = p.scale_log2;
+    const int page = p.c.page, sub_k = col >> 2, key_k = col & 3;
+
+    // The page of 16 keys, -1 where there is none.
+    auto lookup = [&](int key) __attribute__((always_inline)) {
+        int at = -1;
+        if (key < seen.n) at = p.c.table[b * p.c.pitch + (key >> p.c.page_log2)];
+        return at >= 0 && at < p.c.P ? at : -1;
+    };
+    auto tile_of = [&](int t) __attribute__((always_inline)) { return t < seen.sink_tiles ? t : t - seen.sink_tiles + seen.first; };
+
+    for (int t = t0 + wave; t < t1; t += kWaves) {
+        const int key0 = tile_of(t) * kTile;
+        const int at_k = lookup(key0 + 16 * sub_k), at_v = lookup(key0 + 16 * grp);
+        const size_t unit_k = (size_t)max(at_k, 0) * p.c.Hkv + hk, unit_v = (size_t)max(at_v, 0) * p.c.Hkv + hk;
+        const float scale_k = __uint_as_float((unsigned)p.c.ke[unit_k] << 23), scale_v = __uint_as_float((unsigned)p.c.ve[unit_v] << 23);
+        const unsigned char* const kp = p.c.k + unit_k * page * D + (size_t)(((key0 + 16 * sub_k) & (page - 1)) + key_k) * D + 16 * grp;
+        const unsigned char* const vp = p.c.v + unit_v * page * D + col * page + ((key0 + 16 * grp) & (page - 1));
+        u32x4 kr[4][KC], vr[DT];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int ch = 0; ch < KC; ++ch) kr[kt][ch] = *(const u32x4*)(kp + 4 * kt * D + 64 * ch);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) vr[d] = *(const u32x4*)(vp + d * 16 * page);
+
+        // a tile with keys that some row does not see
+        const int key_g = key0 + 16 * grp;                   // this lane's 16 scores are those of keys key_g ...
+        bool edge = at_v < 0;
+#pragma unroll
+        for (int r = 0; r < NR; ++r) edge = edge || key0 + kTile - 1 > hi[r] || (key0 < lo[r] && key0 + kTile > p.sinks);
+        edge = __builtin_amdgcn_ballot_w64(edge) != 0;
+        bool poisoned = false;
+        if (edge) {
+            // codes that no row sees become zero: the product 0 * NaN must not reach a row
+            u32x4 keep = {0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int key = key_g + j;
+                if (at_v >= 0 && key <= hi_all && (key >= lo_all || key < p.sinks)) keep[j / 4] |= 0xffu << (8 * (j % 4));
+            }
+            unsigned bad = 0;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                vr[d] &= keep;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) bad |= nan_codes(vr[d][j]);
+            }
+            poisoned = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
+        }
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            f32x4 sc[4];
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+                sc[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ch = 0; ch < KC; ++ch) {
+                    sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(kr[kt][ch][0], kr[kt][ch][1], scale_k), qf[r][2 * ch], sc[kt], 0, 0, 0);
+                    sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(kr[kt][ch][2], kr[kt][ch][3], scale_k), qf[r][2 * ch + 1], sc[kt], 0, 0, 0);
+                }
+            }
+            unsigned visible = 0xffffu;
+            if (edge) {
+                visible = 0;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int key = key_g + j;
+                    if (at_v >= 0 && key <= hi[r] && (key >= lo[r] || key < p.sinks)) visible |= 1u << j;
+                    else sc[j / 4][j % 4] = -INFINITY;
+                }
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) mx = fmaxf(mx, sc[j / 4][j % 4]);
+            const float m_new = fmaxf(m_run[r], max_over_groups(mx));
+            const float m_use = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = exp2_hw((m_run[r] - m_use) * c), mc = m_use * c;
+            m_run[r] = m_new;
+            float sum = 0.f;
+            unsigned pk[8];
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const float p0 = exp2_hw(fmaf(sc[j / 4][j % 4], c, -mc)), p1 = exp2_hw(fmaf(sc[j / 4][j % 4 + 1], c, -mc));
+                sum += p0 + p1;
+                pk[j / 2] = pack_bf16x2(p0, p1);
+            }
+            l_run[r] = l_run[r] * alpha + sum;
+            if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) oacc[r][d] *= alpha;
+            const bf16x8 pf0 = __builtin_bit_cast(bf16x8, (u32x4{pk[0], pk[1], pk[2], pk[3]}));
+            const bf16x8 pf1 = __builtin_bit_cast(bf16x8, (u32x4{pk[4], pk[5], pk[6], pk[7]}));
+            if (!poisoned) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(vr[d][0], vr[d][1], scale_v), pf0, oacc[r][d], 0, 0, 0);
+                    oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(vr[d][2], vr[d][3], scale_v), pf1, oacc[r][d], 0, 0, 0);
+                }
+            } else {
+                // NaN codes among keys that only some rows see: without them, and then a NaN for every row that sees one
+                bf16x8 see0, see1;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    see0[j] = (__bf16)((visible >> j) & 1 ? 1.f : 0.f);
+                    see1[j] = (__bf16)((visible >> (8 + j)) & 1 ? 1.f : 0.f);
+                }
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    bf16x8 ind[2];
+                    u32x4 w = vr[d];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const unsigned nan = nan_codes(w[j]);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) ind[j / 2][4 * (j % 2) + y] = (__bf16)((nan >> (8 * y + 7)) & 1 ? 1.f : 0.f);
+                        w[j] &= ~((nan >> 7) * 0xffu);
+                    }
+                    f32x4 hits = {0.f, 0.f, 0.f, 0.f};
+                    hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ind[0], see0, hits, 0, 0, 0);
+                    hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ind[1], see1, hits, 0, 0, 0);
+                    oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(w[0], w[1], scale_v), pf0, oacc[r][d], 0, 0, 0);
+                    oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(w[2], w[3], scale_v), pf1, oacc[r][d], 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) oacc[r][d][e] = hits[e] > 0.f ? NAN : oacc[r][d][e];
+                }
+            }
+        }
+    }
+
+    // merge the wavefronts: each scales its O to the maximum over all of them
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const float l = sum_over_groups(l_run[r]);
+        if (grp == 0) { s_ml[0][wave][r * kBlock + col] = m_run[r]; s_ml[1][wave][r * kBlock + col] = l; }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+        const int row = r * kBlock + col;
+        float m = s_ml[0][0][row];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_ml[0][w][row]);
+        const float f = m_run[r] == -INFINITY ? 0.f : exp2_hw((m_run[r] - m) * c);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *(f32x4*)(s_o + (wave * ROWS + row) * PITCH + 16 * d + 4 * grp) = oacc[r][d] * f;
+    }
+    if (tid < ROWS && first + tid < R) {
+        const int row = first + tid, i = row / g, h = row - i * g;
+        const size_t rowi = ((size_t)b * p.Hq + hk * g + h) * p.Sq + i;
+        float m = s_ml[0][0][tid], l = 0.f;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_ml[0][w][tid]);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) l += s_ml[1][w][tid] * (s_ml[0][w][tid] == -INFINITY ? 0.f : exp2_hw((s_ml[0][w][tid] - m) * c));
+        const bool none = l == 0.f || i >= seen.rows;
+        s_inv[tid] = none ? 0.f : 1.f / l;
+        if (p.splits == 1) {
+            if (p.lse) p.lse[rowi] = none ? -INFINITY : m * p.scale + logf(l);
+        } else {
+            *(f32x2*)(p.ml + 2 * (rowi * p.splits + split)) = f32x2{none ? -INFINITY : m, none ? 0.f : l};
+        }
+    }
+    __syncthreads();
+    constexpr int QPR = D / 4;
+    for (int item = tid; item < ROWS * QPR; item += kWaves * 64) {
+        const int rr = item / QPR, d = item % QPR * 4, row = first + rr;
+        if (row >= R) break;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += *(const f32x4*)(s_o + (w * ROWS + rr) * PITCH + d);
+        const int i = row / g, h = row - i * g;
+        if (p.splits == 1) {
+            const float inv = s_inv[rr];
+            u32x2 w2 = {0, 0};
+            if (inv != 0.f) w2 = u32x2{pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv)};
+            *(u32x2*)(p.o + b * p.o_sb + (hk * g + h) * p.o_sh + (long long)i * p.o_ss + d) = w2;
+        } else {
+            *(f32x4*)(p.part + ((((size_t)b * p.Hq + hk * g + h) * p.Sq + i) * p.splits + split) * D + d) = v;
+        }
+    }
+}
+
+// O and LSE of a row from the parts of its splits: one workgroup per row.
+template <int D>
+__global__ __launch_bounds__(256) void attn_kv_combine(KvAttnParams p, int rows_per_wg) {
+    constexpr int QPR = D / 4, NS = 256 / QPR;
+    __shared__ float s_w[kMaxKvSplits];
+    __shared__ float s_red[NS][D];
+    const int tid = threadIdx.x, lane = tid & 63, g = p.Hq / p.c.Hkv;
+    const size_t rowi = blockIdx.x;
+    const int i = (int)(rowi % p.Sq), hq = (int)(rowi / p.Sq % p.Hq), b = (int)(rowi / p.Sq / p.Hq);
+    const int row = i * g + hq % g;
+    const Seen seen = seen_tiles(p, b, g, row / rows_per_wg * rows_per_wg, rows_per_wg);
+    const int per = (seen.count + p.splits - 1) / p.splits;
+    const int S = per > 0 && i < seen.rows ? (seen.count + per - 1) / per : 0;     // splits that left a part
+    float m = -INFINITY, l = 0.f;
+    for (int s = lane; s < S; s += 64) m = fmaxf(m, p.ml[2 * (rowi * p.splits + s)]);
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    for (int s = lane; s < S; s += 64) {
+        const f32x2 ml = *(const f32x2*)(p.ml + 2 * (rowi * p.splits + s));
+        const float w = ml[0] == -INFINITY ? 0.f : exp2_hw((ml[0] - m) * p.scale_log2);
+        l += ml[1] * w;
+        if (tid < 64) s_w[s] = w;
+    }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x);
+    __syncthreads();
+    const int sl = tid / QPR, d = tid % QPR * 4;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int s = sl; s < S; s += NS)
+        acc += *(const f32x4*)(p.part + (rowi * p.splits + s) * D + d) * s_w[s];
+    *(f32x4*)&s_red[sl][d] = acc;
+    __syncthreads();
+    if (tid < D / 2) {
+        float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+        for (int n = 0; n < NS; ++n) { a0 += s_red[n][2 * tid]; a1 += s_red[n][2 * tid + 1]; }
+        const bool none = l == 0.f;
+        const float inv = none ? 0.f : 1.f / l;
+        *(unsigned*)(p.o + b * p.o_sb + hq * p.o_sh + (long long)i * p.o_ss + 2 * tid) = none ? 0u : pack_bf16x2(a0 * inv, a1 * inv);
+        if (tid == 0 && p.lse) p.lse[rowi] = none ? -INFINITY : m * p.scale + logf(l);
+    }
+}
+
+}  // namespace
+
+KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits) {
+    KvAttnPlan plan;
+    const long long R = (long long)(Hq / Hkv) * Sq;
+    plan.rows = kBlock;
+    plan.row_wgs = (int)((R + plan.rows - 1) / plan.rows);
+    plan.splits = splits;
+    if (splits == 0) {
+        const int tiles = (keys + kTile - 1) / kTile, most = (tiles + kWaves - 1) / kWaves;
+        const long long base = (long long)B * Hkv * plan.row_wgs;
+        long long s = 1024 / base;
+        if (s > most) s = most;
+        plan.splits = s < 1 ? 1 : s > kMaxKvSplits ? kMaxKvSplits : (int)s;
+    }
+    (void)D;
+    return plan;
+}
+
+int attn_kv_launch(KvAttnParams p, const KvAttnPlan& plan, hipStream_t stream) {
+    p.row_wgs = plan.row_wgs; p.splits = plan.splits;
+    const double blocks = (double)p.B * p.c.Hkv * p.row_wgs * p.splits;
+    if (blocks * 256 >= 4294967296.0) return -2;
+    const dim3 grid((unsigned)blocks), block(kWaves * 64);
+    if (p.c.D == 128) hipLaunchKernelGGL((attn_kv_rows<128, 1>), grid, block, 0, stream, p);
+    else hipLaunchKernelGGL((attn_kv_rows<64, 1>), grid, block, 0, stream, p);
+    if (hipGetLastError() != hipSuccess) return -1;
+    if (p.splits > 1) {
+        const unsigned rows = (unsigned)p.B * p.Hq * p.Sq;
+        if (p.c.D == 128) hipLaunchKernelGGL(attn_kv_combine<128>, dim3(rows), dim3(256), 0, stream, p, plan.rows);
+        else hipLaunchKernelGGL(attn_kv_combine<64>, dim3(rows), dim3(256), 0, stream, p, plan.rows);
+        if (hipGetLastError() != hipSuccess) return -1;
+    }
+    return 0;
+}
