@@ -83,7 +83,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
     int logical = bid < per_xcd * 8 ? (bid & 7) * per_xcd + (bid >> 3) : bid;
     const int rowblk = logical % p.row_wgs; logical /= p.row_wgs;
     const int split = logical % p.splits; logical /= p.splits;
-    const int hk = logical % p.c.Hkv, b = logical / p.c.Hkv;
+    const int B = p.B, b = logical % B, hk = logical / B;                // (an XCD gets heads, and so sequences of all lengths)
 
     const int g = p.Hq / p.c.Hkv, R = g * p.Sq, first = rowblk * ROWS;
     const Seen seen = seen_tiles(p, b, g, first, ROWS);
@@ -302,6 +302,314 @@ __global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
     }
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// More packed rows than a few blocks: a wavefront owns 32 of them (the columns of v_mfma_f32_32x32x16_bf16), the wavefronts of
+// a workgroup share tiles of 64 keys, which are decoded once, on the way from memory through registers into LDS: K as
+// [64][D] and V^T as [D][64] bf16, two stages of each.  While tile t is worked on, tile t + 1 is decoded and written, tile
+// t + 2 is on its way into registers and the page numbers of tile t + 3 are looked up; one barrier per tile.
+//
+// Row m of a 32-key block of S^T stands for key m with bits 2 and 3 exchanged: then the eight scores that a lane holds for a
+// step of 16 keys are those of eight consecutive keys, one 16-byte piece of its row of V^T.
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr int kTileRows = 32;
+__device__ __forceinline__ constexpr int key_of_row(int m) { return (m & 0x13) | ((m >> 1) & 4) | ((m << 1) & 8); }
+// Rows of K (2 D bytes) and of V^T (128 bytes) in pieces of 16 bytes, their places exchanged so that 16 consecutive rows' reads of
+// one piece hit all banks once (rows of 128 bytes: two of them per turn of the banks).
+template <int PIECES> __device__ __forceinline__ constexpr int piece_offset(int row, int piece) {
+    return row * PIECES * 16 + ((piece ^ (PIECES == 16 ? row & 15 : (row >> 1) & 7)) << 4);
+}
+
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
+    constexpr int KS = D / 16, DB = D / 32, KP = D / 8;
+    constexpr int NC = D * kTile / 16 / (NW * 64);        // 16-code pieces per thread, tile and matrix
+    constexpr int STAGE = 2 * kTile * D * 2;              // bytes of a K and a V tile
+    constexpr int ROWS = NW * kTileRows;
+    __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
+    // by stage, the last tile: whose group of 16 keys has no page; whose V has a NaN, and which (for tiles at an edge only)
+    __shared__ __attribute__((aligned(16))) int s_gone[2][4];
+    __shared__ int s_nan[2];
+    __shared__ __attribute__((aligned(8))) unsigned short s_bits[2][D][4];
+
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int nb = gridDim.x, per_xcd = nb >> 3, bid = blockIdx.x;
+    int logical = bid < per_xcd * 8 ? (bid & 7) * per_xcd + (bid >> 3) : bid;
+    const int rowblk = p.row_wgs - 1 - logical % p.row_wgs; logical /= p.row_wgs;       // (the last rows see the most keys)
+    const int split = logical % p.splits; logical /= p.splits;
+    const int B = p.B, b = logical % B, hk = logical / B;                // (an XCD gets heads, and so sequences of all lengths)
+
+    const int g = p.Hq / p.c.Hkv, R = g * p.Sq, first = rowblk * ROWS;
+    const Seen seen = seen_tiles(p, b, g, first, ROWS);
+    const int per = (seen.count + p.splits - 1) / p.splits;
+    const int t0 = split * per, t1 = min(seen.count, t0 + per);
+    if (p.splits > 1 && t0 >= t1) return;
+
+    // this lane's row; rows past the last one see what it does and are not stored
+    const int row = min(first + wave * kTileRows + (lane & 31), R - 1), row_i = row / g, hq = hk * g + row - row_i * g;
+    const int most_i = max(seen.rows - 1, 0);
+    auto high_of = [&](int i) __attribute__((always_inline)) { return p.causal ? min(seen.pos0 + min(i, most_i), seen.n - 1) : seen.n - 1; };
+    auto low_of = [&](int i) __attribute__((always_inline)) { return p.window ? (int)max((long long)seen.pos0 + min(i, most_i) - p.window + 1, 0LL) : 0; };
+    const int hi = high_of(row_i), lo = low_of(row_i);
+    // its wavefront's and its workgroup's first and last rows
+    const int w_row0 = min(first + wave * kTileRows, R - 1) / g, w_row1 = min(first + wave * kTileRows + kTileRows - 1, R - 1) / g;
+    const int w_hi = high_of(w_row1), w_lo = low_of(w_row0);
+    const int g_hi = high_of(first / g), g_lo = low_of(min(first + ROWS - 1, R - 1) / g);
+
+    // The order of the tiles: those that every row sees whole, a0 ... a1 - 1, then the first tokens', then the others.
+    const int end = seen.first + seen.count - seen.sink_tiles;
+    const int a0 = min(end, max(seen.first, (g_lo + kTile - 1) / kTile)), a1 = max(a0, min(end, (g_hi + 1) / kTile));
+    const int whole = a1 - a0;
+    auto tile_of = [&](int t) __attribute__((always_inline)) {
+        const int x = t - whole, y = x - seen.sink_tiles + seen.first;
+        const int z = x < seen.sink_tiles ? x : y < a0 ? y : y + whole;
+        return t < whole ? a0 + t : z;
+    };
+
+    // A wavefront's pieces lie in one page each: K piece n is key k_key + 8 (D 64: 16) n, codes from 16 k_c on; V piece n the 16
+    // keys of group v_grp, row v_row + 64 n.  So page numbers and addresses are scalars.
+    constexpr int KPI = 1024 / D;                         // keys per load of a wavefront
+    const int page = p.c.page, page_log2 = p.c.page_log2;
+    const int k_first = wave * (kTile / NW), k_key = k_first + lane / (D / 16), k_c = lane % (D / 16);
+    const int v_grp = wave & 3, v_row = (wave >> 2) * NC * 64 + lane;
+    typedef const int __attribute__((address_space(4))) * ScalarInts;
+    const ScalarInts table = (ScalarInts)(p.c.table + b * p.c.pitch);
+    int at_k, at_v;                                       // the pages of the tile that is loaded next, -1: none
+    u32x4 kr[NC], vr[NC];
+    unsigned ke, ve;                                      // biased exponents
+    bool gap;                                             // whether the loaded V piece has no page
+    auto lookup = [&](int key) __attribute__((always_inline)) {
+        const int at = table[min(key, seen.n - 1) >> page_log2];
+        return key < seen.n && (unsigned)at < (unsigned)p.c.P ? at : -1;
+    };
+    auto find = [&](int t) __attribute__((always_inline)) {           // (behind the last tile: the last one again)
+        const int key0 = tile_of(min(t, t1 - 1)) * kTile;
+        at_k = lookup(key0 + k_first);
+        at_v = lookup(key0 + 16 * v_grp);
+    };
+    const unsigned k_lane = lane / (D / 16) * D + 16 * k_c, v_lane = v_row * page;
+    auto load = [&](int t) __attribute__((always_inline)) {
+        const int key0 = tile_of(min(t, t1 - 1)) * kTile;
+        const size_t unit_k = (size_t)max(at_k, 0) * p.c.Hkv + hk, unit_v = (size_t)max(at_v, 0) * p.c.Hkv + hk;
+        const unsigned char* const k = p.c.k + (unit_k * page + ((key0 + k_first) & (page - 1))) * D;
+        const unsigned char* const v = p.c.v + unit_v * page * D + ((key0 + 16 * v_grp) & (page - 1));
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            kr[n] = *(const u32x4*)(k + k_lane + n * KPI * D);
+            vr[n] = *(const u32x4*)(v + v_lane + n * 64 * page);
+        }
+        ke = p.c.ke[unit_k];
+        ve = p.c.ve[unit_v];
+        gap = at_v < 0;
+    };
+    // What tile t, loaded, needs before it is decoded: zeros where the sequence holds nothing, a note of groups without a page.
+    // At an edge NaN must not meet the probability 0 of a row that does not see it: zeros too, and a note.
+    auto mend = [&](int t) __attribute__((always_inline)) {
+        if (t < whole && !gap) return;
+        const int key0 = tile_of(min(t, t1 - 1)) * kTile, left = gap ? 0 : seen.n - (key0 + 16 * v_grp);
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            unsigned bits = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int bytes = min(max(left - 4 * j, 0), 4);
+                unsigned w = vr[n][j] & (bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1);
+                const unsigned nan = nan_codes(w) >> 7;
+                if (t >= whole) w &= ~(nan * 0xffu);
+                bits |= (nan * 0x10204080u >> 28) << (4 * j);                         // bytes 0 ... 3 to bits 0 ... 3
+                vr[n][j] = w;
+            }
+            if (t >= whole) {
+                s_bits[t & 1][v_row + 64 * n][v_grp] = (unsigned short)bits;
+                if (bits) s_nan[t & 1] = t;
+            }
+        }
+        if (gap) s_gone[t & 1][v_grp] = t;
+    };
+    // Lane offsets into a stage; the pieces of a row are found by exchanging address bits.
+    unsigned k_read = piece_offset<KP>(key_of_row(lane & 31), half), v_read = kTile * D * 2 + piece_offset<8>(lane & 31, half);
+    unsigned k_write = piece_offset<KP>(k_key, 2 * k_c), v_write = kTile * D * 2 + piece_offset<8>(v_row, 2 * v_grp);
+    auto put = [&](int t) __attribute__((always_inline)) {
+        const unsigned st = (t & 1) * STAGE;
+        const float ks = __uint_as_float(ke << 23), vs = __uint_as_float(ve << 23);
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            // (K rows n KPI further on: for D = 128 their pieces' places differ in bit 3)
+            const unsigned kw = (k_write ^ (KP == 16 && (n & 1) ? 128u : 0u)) + st + n * KPI * D * 2;
+            *(bf16x8*)(smem + kw) = decode(kr[n][0], kr[n][1], ks);
+            *(bf16x8*)(smem + (kw ^ 16)) = decode(kr[n][2], kr[n][3], ks);
+            *(bf16x8*)(smem + (v_write + st + n * 64 * 128)) = decode(vr[n][0], vr[n][1], vs);
+            *(bf16x8*)(smem + ((v_write + st + n * 64 * 128) ^ 16)) = decode(vr[n][2], vr[n][3], vs);
+        }
+    };
+    auto barrier = [&]() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    bf16x8 qf[KS];
+    {
+        const __bf16* const q = p.q + b * p.q_sb + hq * p.q_sh + (long long)min(row_i, most_i) * p.q_ss + 8 * half;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qf[s] = *(const bf16x8*)(q + 16 * s);
+    }
+    f32x16 oacc[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oacc[i][e] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    const float c = p.scale_log2;
+
+    f32x16 sc[2];
+    bf16x8 pf[4];
+    auto scores = [&](int t) __attribute__((always_inline)) {
+        const unsigned at = k_read + (t & 1) * STAGE;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[kb][e] = 0.f;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bf16x8 kf = *(const bf16x8*)(smem + (at ^ (s << 5)) + 32 * kb * D * 2);
+                sc[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], sc[kb], 0, 0, 0);
+            }
+        }
+    };
+    auto softmax = [&]() __attribute__((always_inline)) {
+        float mx = sc[0][0];
+#pragma unroll
+        for (int j = 1; j < 32; ++j) mx = fmaxf(mx, sc[j / 16][j % 16]);
+        const float m_new = fmaxf(m_run, max_across_halves(mx));
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = exp2_hw((m_run - m_use) * c), mc = m_use * c;
+        m_run = m_new;
+        float sum = 0.f;
+        unsigned pk[16];
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            const float p0 = exp2_hw(fmaf(sc[j / 16][j % 16], c, -mc)), p1 = exp2_hw(fmaf(sc[j / 16][j % 16 + 1], c, -mc));
+            sum += p0 + p1;
+            pk[j / 2] = pack_bf16x2(p0, p1);
+        }
+        l_run = l_run * alpha + sum;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) pf[kk] = __builtin_bit_cast(bf16x8, (u32x4{pk[4 * kk], pk[4 * kk + 1], pk[4 * kk + 2], pk[4 * kk + 3]}));
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0)
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) oacc[i][e] *= alpha;
+    };
+    auto weigh = [&](int t) __attribute__((always_inline)) {
+        const unsigned at = v_read + (t & 1) * STAGE;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                const bf16x8 vf = *(const bf16x8*)(smem + (at ^ (kk << 5)) + 32 * i * 128);
+                oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[kk], oacc[i], 0, 0, 0);
+            }
+    };
+    // a NaN for every row that sees one
+    auto poison = [&](int t, unsigned visible) __attribute__((always_inline)) {
+        for (int d = 0; d < D; ++d) {
+            const u32x2 bits = *(const u32x2*)s_bits[t & 1][d];
+            const unsigned b0 = __builtin_amdgcn_readfirstlane(bits[0]) >> (8 * half), b1 = __builtin_amdgcn_readfirstlane(bits[1]) >> (8 * half);
+            if (__builtin_amdgcn_readfirstlane(bits[0] | bits[1]) == 0) continue;
+            unsigned mine = visible & ((b0 & 0xff) | (b0 >> 8 & 0xff00) | (b1 & 0xff) << 16 | (b1 >> 8 & 0xff00) << 16);
+            mine |= __shfl_xor(mine, 32);
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) oacc[i][e] = mine != 0 && d == 32 * i + 8 * (e / 4) + 4 * half + e % 4 ? NAN : oacc[i][e];
+        }
+    };
+    // which of the 32 keys of this lane's scores its row sees
+    auto seen_keys = [&](int key0, unsigned there) __attribute__((always_inline)) {
+        auto upto = [](int n) __attribute__((always_inline)) { return (1u << min(max(n, 0), 8)) - 1; };
+        unsigned visible = 0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int key = key0 + 16 * x + 8 * half;
+            const unsigned bits = upto(hi - key + 1) & (~upto(lo - key) | upto(p.sinks - key));
+            visible |= (there >> x & 1 ? bits & 0xff : 0) << (8 * x);
+        }
+        return visible;
+    };
+
+    if (t0 < t1) {
+        if (tid < 8) { s_nan[tid & 1] = -1; s_gone[tid & 1][tid >> 1] = -1; }
+        find(t0); load(t0); find(t0 + 1);
+        barrier();
+        mend(t0); put(t0); load(t0 + 1); find(t0 + 2);
+        barrier();
+    }
+    auto groups = [&](int t) __attribute__((always_inline)) {                // which groups of 16 keys have a page
+        const i32x4 gone = *(const i32x4*)s_gone[t & 1];
+        unsigned there = 15;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) if (__builtin_amdgcn_readfirstlane(gone[x]) == t) there &= ~(1u << x);
+        return there;
+    };
+    int t = t0;
+    for (; t < min(t1, whole); ++t) {
+        asm volatile("" : "+v"(k_read), "+v"(v_read), "+v"(k_write), "+v"(v_write));     // (offsets are cheaper to make again than to keep)
+        if (groups(t) != 15) break;                                          // a page is missing: the general loop goes on
+        mend(t + 1);
+        scores(t);
+        put(t + 1); load(t + 2); find(t + 3);
+        softmax();
+        weigh(t);
+        barrier();
+    }
+    for (; t < t1; ++t) {
+        asm volatile("" : "+v"(k_read), "+v"(v_read), "+v"(k_write), "+v"(v_write));
+        const int key0 = tile_of(t) * kTile;
+        const unsigned there = groups(t);
+        mend(t + 1);
+        put(t + 1); load(t + 2); find(t + 3);
+        // nothing for this wavefront behind its last row's position, or in front of its first row's window
+        if (key0 <= w_hi && (key0 + kTile > w_lo || key0 < p.sinks)) {
+            scores(t);
+            const unsigned visible = seen_keys(key0, there);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sc[j / 16][j % 16] = visible >> j & 1 ? sc[j / 16][j % 16] : -INFINITY;
+            softmax();
+            weigh(t);
+            if (__builtin_amdgcn_readfirstlane(s_nan[t & 1]) == t) poison(t, visible);
+        }
+        barrier();
+    }
+
+    const float l = sum_across_halves(l_run);
+    const int r = first + wave * kTileRows + (lane & 31);
+    if (r >= R) return;
+    const size_t rowi = ((size_t)b * p.Hq + hq) * p.Sq + row_i;
+    const bool none = l == 0.f || row_i >= seen.rows;
+    if (p.splits == 1) {
+        const float inv = none ? 0.f : 1.f / l;
+        __bf16* const o = p.o + b * p.o_sb + hq * p.o_sh + (long long)row_i * p.o_ss;
+#pragma unroll
+        for (int x = 0; x < DB; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const u32x2 w = {pack_bf16x2(oacc[x][4 * y] * inv, oacc[x][4 * y + 1] * inv), pack_bf16x2(oacc[x][4 * y + 2] * inv, oacc[x][4 * y + 3] * inv)};
+                *(u32x2*)(o + 32 * x + 8 * y + 4 * half) = none ? u32x2{0, 0} : w;
+            }
+        if (half == 0 && p.lse) p.lse[rowi] = none ? -INFINITY : m_run * p.scale + logf(l);
+    } else {
+        float* const o = p.part + (rowi * p.splits + split) * D;
+#pragma unroll
+        for (int x = 0; x < DB; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) *(f32x4*)(o + 32 * x + 8 * y + 4 * half) = f32x4{oacc[x][4 * y], oacc[x][4 * y + 1], oacc[x][4 * y + 2], oacc[x][4 * y + 3]};
+        if (half == 0) *(f32x2*)(p.ml + 2 * (rowi * p.splits + split)) = f32x2{none ? -INFINITY : m_run, none ? 0.f : l};
+    }
+}
+
 // O and LSE of a row from the parts of its splits: one workgroup per row.
 template <int D>
 __global__ __launch_bounds__(256) void attn_kv_combine(KvAttnParams p, int rows_per_wg) {
@@ -347,30 +655,37 @@ __global__ __launch_bounds__(256) void attn_kv_combine(KvAttnParams p, int rows_
 
 }  // namespace
 
+constexpr int tile_waves(int D) { return D == 128 ? 4 : 4; }
+
+// Rows per workgroup: 16 where that is all there is, else 32 rows per wavefront that share decoded tiles.
 KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits) {
     KvAttnPlan plan;
     const long long R = (long long)(Hq / Hkv) * Sq;
-    plan.rows = kBlock;
+    plan.rows = R <= kBlock ? kBlock : tile_waves(D) * kTileRows;
     plan.row_wgs = (int)((R + plan.rows - 1) / plan.rows);
     plan.splits = splits;
     if (splits == 0) {
-        const int tiles = (keys + kTile - 1) / kTile, most = (tiles + kWaves - 1) / kWaves;
+        const int tiles = (keys + kTile - 1) / kTile, most = plan.rows == kBlock ? (tiles + kWaves - 1) / kWaves : (tiles + 3) / 4;
         const long long base = (long long)B * Hkv * plan.row_wgs;
-        long long s = 1024 / base;
+        long long s = (plan.rows == kBlock ? 1024 : 512) / base;
         if (s > most) s = most;
         plan.splits = s < 1 ? 1 : s > kMaxKvSplits ? kMaxKvSplits : (int)s;
     }
-    (void)D;
     return plan;
+}
+
+template <int D>
+static void launch(const KvAttnParams& p, const KvAttnPlan& plan, unsigned blocks, hipStream_t stream) {
+    if (plan.rows == kBlock) hipLaunchKernelGGL((attn_kv_rows<D, 1>), dim3(blocks), dim3(kWaves * 64), 0, stream, p);
+    else hipLaunchKernelGGL((attn_kv_tiles<D, tile_waves(D)>), dim3(blocks), dim3(tile_waves(D) * 64), 0, stream, p);
 }
 
 int attn_kv_launch(KvAttnParams p, const KvAttnPlan& plan, hipStream_t stream) {
     p.row_wgs = plan.row_wgs; p.splits = plan.splits;
     const double blocks = (double)p.B * p.c.Hkv * p.row_wgs * p.splits;
-    if (blocks * 256 >= 4294967296.0) return -2;
-    const dim3 grid((unsigned)blocks), block(kWaves * 64);
-    if (p.c.D == 128) hipLaunchKernelGGL((attn_kv_rows<128, 1>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((attn_kv_rows<64, 1>), grid, block, 0, stream, p);
+    if (blocks * 512 >= 4294967296.0) return -2;
+    if (p.c.D == 128) launch<128>(p, plan, (unsigned)blocks, stream);
+    else launch<64>(p, plan, (unsigned)blocks, stream);
     if (hipGetLastError() != hipSuccess) return -1;
     if (p.splits > 1) {
         const unsigned rows = (unsigned)p.B * p.Hq * p.Sq;
