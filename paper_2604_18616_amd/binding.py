@@ -126,7 +126,8 @@ def _load_native():
     if module:
         module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
             lib.attn_fwd, lib.attn_fwd_strided, lib.attn_fwd_workspace_bytes, lib.attn_fwd_workspace,
-            lib.gemm_bf16_workspace_bytes, lib.gemm_bf16_tile, lib.gemm_bf16_workspace)))
+            lib.gemm_bf16_workspace_bytes, lib.gemm_bf16_tile, lib.gemm_bf16_workspace,
+            lib.kv_fp8_write, lib.kv_fp8_read, lib.attn_kv_fp8_workspace_bytes, lib.attn_kv_fp8, lib.rope_bf16)))
     _native = module
     return module
 
@@ -439,11 +440,39 @@ def _rows(t, shape, device, name):
     return _strides3(t)
 
 
+def _done(answer):
+    """What a call of the extension module returned, an error code raised."""
+    if type(answer) is int:
+        raise AttnError(answer, strerror(answer))
+    return answer
+
+
+class _on:
+    """Launches for tensors on another device than the current one, on that device."""
+
+    def __init__(self, device):
+        import torch
+        self.guard = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *why):
+        if self.guard is not None:
+            self.guard.__exit__(*why)
+
+
 def kv_fp8_write(cache, k, v, table, start, count=None, stream=None):
     """Append k, v (bf16 [B, Hkv, S, D], strided views as in attn_fwd) to a quantised cache: token t of sequence b, t < count[b]
     (all where count is None), goes to position start[b] + t, which lies on page table[b][position // page].  table int32
     [B, width], start and count int32 [B], all on the GPU.  Enqueued on `stream` (default: torch's current stream); no sync.
     Returns the cache."""
+    if stream is None:
+        native = _plain_calls(k)
+        done = native.kv_write(cache, k, v, table, start, count) if native else None      # None: not a plain call
+        if done is not None:
+            return _done(done)
     struct, H, D, device = _cache_struct(cache)
     at, pitch, B, width = _table(table, device)
     if k.dim() != 4:
@@ -451,8 +480,9 @@ def kv_fp8_write(cache, k, v, table, start, count=None, stream=None):
     S = k.shape[2]
     ks, vs = (_rows(t, (B, H, S, D), device, name) for t, name in ((k, "k"), (v, "v")))
     stream, _ = _streams(k, stream)
-    rc = load_library().kv_fp8_write(ctypes.byref(struct), k.data_ptr(), v.data_ptr(), ks, vs, at, pitch, width,
-                                     _per_sequence(start, B, device, "start"), _per_sequence(count, B, device, "count"), B, S, stream)
+    start, count = _per_sequence(start, B, device, "start"), _per_sequence(count, B, device, "count")
+    with _on(device):
+        rc = load_library().kv_fp8_write(ctypes.byref(struct), k.data_ptr(), v.data_ptr(), ks, vs, at, pitch, width, start, count, B, S, stream)
     if rc != 0:
         raise AttnError(rc, strerror(rc))
     return cache
@@ -461,6 +491,11 @@ def kv_fp8_write(cache, k, v, table, start, count=None, stream=None):
 def kv_fp8_read(cache, table, lens, S, first=0, k=None, v=None, stream=None):
     """k, v (bf16 [B, Hkv, S, D]) of positions first ... first + S - 1 of every sequence, zeros at positions from lens[b] on and
     on missing pages.  k and v are allocated with torch if not given.  Enqueued on `stream` (default: torch's current stream); no sync."""
+    if k is None and v is None and stream is None:
+        native = _plain_calls(cache[0])
+        done = native.kv_read(cache, table, lens, S, first) if native else None
+        if done is not None:
+            return _done(done)
     import torch
     struct, H, D, device = _cache_struct(cache)
     at, pitch, B, width = _table(table, device)
@@ -469,8 +504,9 @@ def kv_fp8_read(cache, table, lens, S, first=0, k=None, v=None, stream=None):
     v = torch.empty(shape, dtype=torch.bfloat16, device=device) if v is None else v
     ks, vs = (_rows(t, shape, device, name) for t, name in ((k, "k"), (v, "v")))
     stream, _ = _streams(k, stream)
-    rc = load_library().kv_fp8_read(ctypes.byref(struct), at, pitch, width, _per_sequence(lens, B, device, "lens"),
-                                    k.data_ptr(), v.data_ptr(), ks, vs, B, int(S), int(first), stream)
+    lens = _per_sequence(lens, B, device, "lens")
+    with _on(device):
+        rc = load_library().kv_fp8_read(ctypes.byref(struct), at, pitch, width, lens, k.data_ptr(), v.data_ptr(), ks, vs, B, int(S), int(first), stream)
     if rc != 0:
         raise AttnError(rc, strerror(rc))
     return k, v
@@ -482,6 +518,11 @@ def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=Fal
     those only the last `window` and the sequence's `sinks` first.  Rows that see nothing and rows from q_lens[b] on get O = 0
     and LSE = -inf.  lens, q_lens int32 [B] on the GPU; max_len: no sequence is longer (0: the table's width).
     o and lse as in attn_fwd.  Enqueued on `stream` (default: torch's current stream); no sync."""
+    if o is None and lse is None and stream is None:
+        native = _plain_calls(q)
+        done = native.attn_kv(q, cache, table, lens, q_lens, causal, window, sinks, scale, max_len) if native else None
+        if done is not None:
+            return _done(done)
     import torch
     struct, H, D, device = _cache_struct(cache)
     at, pitch, B, width = _table(table, device)
@@ -505,8 +546,9 @@ def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=Fal
     most = width * struct.page
     need = lib.attn_kv_fp8_workspace_bytes(B, Hq, H, Sq, min(max_len, most) if max_len > 0 else most, D, window, sinks) if own else 0
     ws = _scratch(need, device) if need else None
-    rc = lib.attn_kv_fp8(q.data_ptr(), ctypes.byref(struct), at, pitch, width, lens, q_lens, o.data_ptr(), lse.data_ptr(), B, Hq, Sq, qs, os_,
-                         1 if causal else 0, window, sinks, scale, max_len, None if ws is None else ws.data_ptr(), need if ws is not None else 0, 0, stream)
+    with _on(device):
+        rc = lib.attn_kv_fp8(q.data_ptr(), ctypes.byref(struct), at, pitch, width, lens, q_lens, o.data_ptr(), lse.data_ptr(), B, Hq, Sq, qs, os_,
+                             1 if causal else 0, window, sinks, scale, max_len, None if ws is None else ws.data_ptr(), need if ws is not None else 0, 0, stream)
     if rc != 0:
         raise AttnError(rc, strerror(rc))
     return o, lse
@@ -531,6 +573,11 @@ def rope_bf16(q, positions, inv_freq, k=None, q_out=None, k_out=None, interleave
     interleaved: pairs are neighbouring columns, else the halves of the rotated part; inverse: the opposite angle (the
     gradient).  Outputs are allocated with torch if not given and may be the inputs.  Returns q_out, or (q_out, k_out) with k.
     Enqueued on `stream` (default: torch's current stream); no sync."""
+    if q_out is None and k_out is None and stream is None:
+        native = _plain_calls(q)
+        done = native.rope(q, positions, inv_freq, k, interleaved, inverse, scale) if native else None
+        if done is not None:
+            return _done(done)
     import torch
     if not q.is_cuda:
         raise ValueError("q must be a CUDA tensor: there is no CPU path")
@@ -553,9 +600,10 @@ def rope_bf16(q, positions, inv_freq, k=None, q_out=None, k_out=None, interleave
     if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.device != device:
         raise ValueError("inv_freq must be a contiguous float64 vector on q's device")
     stream, _ = _streams(q, stream)
-    rc = load_library().rope_bf16(q.data_ptr(), q_out.data_ptr(), k.data_ptr() if Hk else None, k_out.data_ptr() if Hk else None, B, Hq, Hk, S, D,
-                                  2 * inv_freq.numel(), qs, qos, ks, kos, positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0,
-                                  inv_freq.data_ptr(), 1 if interleaved else 0, 1 if inverse else 0, float(scale), stream)
+    with _on(device):
+        rc = load_library().rope_bf16(q.data_ptr(), q_out.data_ptr(), k.data_ptr() if Hk else None, k_out.data_ptr() if Hk else None, B, Hq, Hk, S, D,
+                                      2 * inv_freq.numel(), qs, qos, ks, kos, positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0,
+                                      inv_freq.data_ptr(), 1 if interleaved else 0, 1 if inverse else 0, float(scale), stream)
     if rc != 0:
         raise AttnError(rc, strerror(rc))
     return q_out if k is None else (q_out, k_out)
