@@ -1,7 +1,4 @@
-// Writing the quantised cache and reading it back, for gfx950.
-//
-// A workgroup owns the keys or the values of one page and kv head, so the page's exponent, its earlier tokens' codes and
-// its new ones are one workgroup's business.  What bounds both: reading and writing every value once.
+// Writing the quantised cache and reading it back, for gfx950.  What bounds both: reading and writing every value once.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -14,13 +11,13 @@ using namespace gfx950;
 
 constexpr int kThreads = 256;
 constexpr int kLeastExp = -100;
+constexpr int kReadRows = 64;        // positions per workgroup of kv_read
 
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }    // -126 <= e <= 127
 __device__ __forceinline__ unsigned char to_e4m3(float x) {
     return (unsigned char)(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);
 }
 __device__ __forceinline__ float from_e4m3(unsigned char c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
-__device__ __forceinline__ float bf16_bits(unsigned short b) { return __uint_as_float((unsigned)b << 16); }
 
 // The least e >= kLeastExp with amax <= 448 * 2^e = 1.75 * 2^(e + 8).
 __device__ __forceinline__ int exponent_for(float amax) {
@@ -29,120 +26,280 @@ __device__ __forceinline__ int exponent_for(float amax) {
     return e < kLeastExp ? kLeastExp : e;
 }
 
-template <int D>
+// Eight codes of x * f; NaN and infinities are 0x7f.  w: eight bf16 bit patterns in four dwords.
+__device__ __forceinline__ u32x2 codes_of(u32x4 w, float f) {
+    u32x2 out;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float x0 = __uint_as_float(w[2 * j] << 16), x1 = __uint_as_float(w[2 * j] & 0xffff0000u);
+        const float x2 = __uint_as_float(w[2 * j + 1] << 16), x3 = __uint_as_float(w[2 * j + 1] & 0xffff0000u);
+        unsigned c = __builtin_amdgcn_cvt_pk_fp8_f32(x0 * f, x1 * f, 0, false);
+        c = __builtin_amdgcn_cvt_pk_fp8_f32(x2 * f, x3 * f, c, true);
+        const unsigned odd = (fabsf(x0) < INFINITY ? 0u : 0xffu) | (fabsf(x1) < INFINITY ? 0u : 0xff00u) |
+                             (fabsf(x2) < INFINITY ? 0u : 0xff0000u) | (fabsf(x3) < INFINITY ? 0u : 0xff000000u);
+        out[j] = (c & ~odd) | (0x7f7f7f7fu & odd);
+    }
+    return out;
+}
+// The largest finite |x| of eight values, as the bits of a bf16 (which order as the values do).
+__device__ __forceinline__ unsigned largest(u32x4 w, unsigned m) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const unsigned lo = w[j] & 0x7fffu, hi = w[j] >> 16 & 0x7fffu;
+        m = max(m, lo < 0x7f80u ? lo : 0u);
+        m = max(m, hi < 0x7f80u ? hi : 0u);
+    }
+    return m;
+}
+
+// A unit is the keys or the values of one page and kv head, so that the page's exponent, its earlier tokens' codes and its new
+// ones are one unit's business: TPU = 64 threads for pages of up to 32 tokens, 256 for larger ones.  A thread reads blocks of 4
+// tokens x 8 values, once, keeps them while the page's maximum is found, and packs the codes of V by four tokens: the transposed
+// page is put together in LDS and leaves in pieces of 16 tokens.
+template <int D, int PAGE>
 __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
-    constexpr int CPR = D / 8;
-    __shared__ float s_max[kThreads / 64];
-    const int tid = threadIdx.x, page = p.c.page;
+    constexpr int TPU = PAGE <= 32 ? 64 : 256, UNITS = kThreads / TPU;
+    constexpr int CPR = D / 8, BLOCKS = PAGE / 4 * CPR, NB = (BLOCKS + TPU - 1) / TPU;
+    constexpr int PITCH = PAGE / 4 + 1;                                // dwords per row d of the page in LDS
+    __shared__ unsigned s_page[UNITS][D * PITCH];
+    __shared__ unsigned s_max[kThreads / 64];
+    const int tid = threadIdx.x % TPU, sub = UNITS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPU);
     const bool is_v = blockIdx.y != 0;
-    unsigned id = blockIdx.x;
+    unsigned id = blockIdx.x * UNITS + sub;
     const int h = id % (unsigned)p.c.Hkv; id /= (unsigned)p.c.Hkv;
     const int f = id % (unsigned)p.F, b = id / (unsigned)p.F;
 
-    const long long start = p.start[b];
-    const int n = p.count ? min(max(p.count[b], 0), p.S) : p.S;
-    const long long pg = (start >> p.c.page_log2) + f;                 // (arithmetic shift: rounds down)
-    if (pg < 0 || pg >= p.c.W) return;
-    const long long base = pg << p.c.page_log2;                        // the page's first position
-    const long long lo = start > base ? start : base, hi = start + n < base + page ? start + n : base + page;
-    if (lo >= hi) return;
-    const int at = p.c.table[b * p.c.pitch + pg];
-    if (at < 0 || at >= p.c.P) return;
-
-    const int held = (int)(lo - base), fresh = (int)(hi - lo);         // earlier tokens of the page, new ones
-    const __bf16* src = is_v ? p.v + b * p.v_sb + h * p.v_sh + (lo - start) * p.v_ss : p.k + b * p.k_sb + h * p.k_sh + (lo - start) * p.k_ss;
-    const long long row = is_v ? p.v_ss : p.k_ss;
-    const size_t unit = (size_t)at * p.c.Hkv + h;
-    unsigned char* const codes = (is_v ? p.c.v : p.c.k) + unit * page * D;
-    unsigned char* const exps = (is_v ? p.c.ve : p.c.ke) + unit;
-
-    float amax = 0.f;
-    for (int i = tid; i < fresh * CPR; i += kThreads) {
-        const s16x8 x = *(const s16x8*)(src + (i / CPR) * row + (i % CPR) * 8);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float a = fabsf(bf16_bits((unsigned short)x[j]));
-            if (a < INFINITY) amax = fmaxf(amax, a);
+    // the unit's tokens: `held` earlier ones of the page, then `fresh` new ones; none where there is nothing to do
+    int held = 0, fresh = 0, at = -1;
+    long long token0 = 0;                                              // of the new ones, the first
+    if (b < p.B) {
+        const long long start = p.start[b];
+        const int n = p.count ? min(max(p.count[b], 0), p.S) : p.S;
+        const long long pg = (start >> p.c.page_log2) + f;             // (arithmetic shift: rounds down)
+        const long long base = pg << p.c.page_log2;                    // the page's first position
+        const long long lo = start > base ? start : base, hi = start + n < base + PAGE ? start + n : base + PAGE;
+        if (pg >= 0 && pg < p.c.W && lo < hi) {
+            at = p.c.table[b * p.c.pitch + pg];
+            if (at >= 0 && at < p.c.P) { held = (int)(lo - base); fresh = (int)(hi - lo); token0 = lo - start; }
         }
     }
+    if (TPU == 256 && fresh == 0) return;
+    const size_t unit = (size_t)(fresh ? at : 0) * p.c.Hkv + h;
+    unsigned char* const codes = (is_v ? p.c.v : p.c.k) + unit * PAGE * D;
+    unsigned char* const exps = (is_v ? p.c.ve : p.c.ke) + unit;
+    const long long row = is_v ? p.v_ss : p.k_ss;
+    const __bf16* const src = (is_v ? p.v + b * p.v_sb + h * p.v_sh : p.k + b * p.k_sb + h * p.k_sh) + (token0 - held) * row;   // of token 0 of the page
+
+    u32x4 x[NB][4];
+    unsigned m = 0;
 #pragma unroll
-    for (int x = 32; x > 0; x >>= 1) amax = fmaxf(amax, __shfl_xor(amax, x));
-    if ((tid & 63) == 0) s_max[tid >> 6] = amax;
-    const int e_old = (int)*exps - 127;
-    __syncthreads();
-    amax = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-    int e = exponent_for(amax);
+    for (int n = 0; n < NB; ++n) {
+        const int blk = n * TPU + tid, q = blk / CPR, c = blk % CPR;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int t = 4 * q + j;
+            x[n][j] = u32x4{0, 0, 0, 0};
+            if (t >= held && t < held + fresh) x[n][j] = *(const u32x4*)(src + t * row + c * 8);
+        }
+    }
+    int e_old = fresh ? (int)*exps - 127 : 0;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = largest(x[n][j], m);
+#pragma unroll
+    for (int y = 32; y > 0; y >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, y));
+    if constexpr (TPU == 256) {
+        if ((tid & 63) == 0) s_max[tid >> 6] = m;
+        __syncthreads();                                               // (and every thread has read the old exponent)
+        m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+    }
+    int e = exponent_for(__uint_as_float(m << 16));
     if (held > 0 && e < e_old) e = e_old;
 
-    auto code_at = [&](int token, int d) { return codes + (is_v ? (size_t)d * page + token : (size_t)token * D + d); };
-    if (held > 0 && e > e_old) {
+    // a scale that has grown: the earlier tokens' codes are rounded again
+    if (held > 0 && fresh > 0 && e > e_old) {
         const float f2 = two_to(max(e_old - e, -126));
-        for (int i = tid; i < held * D; i += kThreads) {
-            unsigned char* const c = code_at(i / D, i % D);
+        for (int i = tid; i < held * D; i += TPU) {
+            unsigned char* const c = codes + (is_v ? (i / held) * PAGE + i % held : i);
             if ((*c & 0x7f) != 0x7f) *c = to_e4m3(from_e4m3(*c) * f2);
         }
     }
     const float f1 = two_to(-e);
-    for (int i = tid; i < fresh * CPR; i += kThreads) {
-        const s16x8 x = *(const s16x8*)(src + (i / CPR) * row + (i % CPR) * 8);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float a = bf16_bits((unsigned short)x[j]);
-            *code_at(held + i / CPR, (i % CPR) * 8 + j) = fabsf(a) < INFINITY ? to_e4m3(a * f1) : (unsigned char)0x7f;
+    for (int n = 0; n < NB; ++n) {
+        const int blk = n * TPU + tid, q = blk / CPR, c = blk % CPR;
+        if (BLOCKS % TPU != 0 && blk >= BLOCKS) break;
+        u32x2 w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = codes_of(x[n][j], f1);
+        if (!is_v) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int t = 4 * q + j;
+                if (t >= held && t < held + fresh) *(u32x2*)(codes + t * D + c * 8) = w[j];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int s = 8 * (i % 4);
+                s_page[sub][(c * 8 + i) * PITCH + q] = (w[0][i / 4] >> s & 0xff) | (w[1][i / 4] >> s & 0xff) << 8 | (w[2][i / 4] >> s & 0xff) << 16 | (w[3][i / 4] >> s & 0xff) << 24;
+            }
         }
     }
-    if (tid == 0) *exps = (unsigned char)(e + 127);
+    if (is_v) {
+        if constexpr (TPU == 256) __syncthreads();
+        else {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (a wavefront reads what it wrote itself)
+            __builtin_amdgcn_wave_barrier();
+        }
+        for (int i = tid; i < D * (PAGE / 16); i += TPU) {
+            const int d = i / (PAGE / 16), t = i % (PAGE / 16) * 16;
+            if (t + 16 <= held || t >= held + fresh) continue;
+            u32x4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = s_page[sub][d * PITCH + t / 4 + j];
+            if (t >= held && t + 16 <= held + fresh) *(u32x4*)(codes + d * PAGE + t) = w;
+            else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (t + j >= held && t + j < held + fresh) codes[d * PAGE + t + j] = (unsigned char)(w[j / 4] >> (8 * (j % 4)));
+            }
+        }
+    }
+    if (tid == 0 && fresh > 0) *exps = (unsigned char)(e + 127);
 }
 
+// Sixteen codes as bf16, times scale: eight dwords of two.
+__device__ __forceinline__ void decode16(u32x4 c, float scale, unsigned (&out)[8]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        out[2 * j] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[j], scale, false));
+        out[2 * j + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[j], scale, true));
+    }
+}
+
+// 64 positions of one sequence and kv head, keys (blockIdx.y 0) or values.  Keys go straight through; a thread with values holds
+// 16 tokens of two columns, which meet their rows in LDS (dword c of the rows of group g lies at c ^ 16 g: no bank conflicts).
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv_read(KvReadParams p) {
-    constexpr int CPR = D / 8;
-    const int page = p.c.page;
-    const bool is_v = blockIdx.y != 0;
-    const size_t idx = (size_t)blockIdx.x * kThreads + threadIdx.x;
-    const int ch = idx % CPR;
-    size_t r = idx / CPR;
-    if (r >= (size_t)p.B * p.c.Hkv * p.S) return;
-    const int s = r % (unsigned)p.S; r /= (unsigned)p.S;
-    const int h = r % (unsigned)p.c.Hkv, b = r / (unsigned)p.c.Hkv;
-    const long long pos = (long long)p.first + s;
-    u32x4 w = {0, 0, 0, 0};
-    if (pos < p.lens[b] && (pos >> p.c.page_log2) < p.c.W) {
+    constexpr int CPR = D / 16, NK = kReadRows * CPR / kThreads;
+    __shared__ __attribute__((aligned(16))) unsigned s_rows[kReadRows * D / 2];
+    const int tid = threadIdx.x, page = p.c.page;
+    const unsigned tiles = (unsigned)((p.S + kReadRows - 1) / kReadRows);
+    unsigned id = blockIdx.x;
+    const int s0 = (int)(id % tiles) * kReadRows; id /= tiles;
+    const int h = id % (unsigned)p.c.Hkv, b = id / (unsigned)p.c.Hkv;
+    const int n = p.lens[b];
+    // a position's codes' page, -1 where there is none
+    auto lookup = [&](long long pos) __attribute__((always_inline)) {
+        if (pos >= n || (pos >> p.c.page_log2) >= p.c.W) return -1;
         const int at = p.c.table[b * p.c.pitch + (pos >> p.c.page_log2)];
-        if (at >= 0 && at < p.c.P) {
-            const size_t unit = (size_t)at * p.c.Hkv + h;
-            const unsigned char* const codes = (is_v ? p.c.v : p.c.k) + unit * page * D;
-            const int token = (int)(pos & (page - 1));
-            const int e = (int)(is_v ? p.c.ve : p.c.ke)[unit] - 127;
-            float x[8];
+        return at >= 0 && at < p.c.P ? at : -1;
+    };
+    if (blockIdx.y == 0) {
+        __bf16* const out = p.k + b * p.k_sb + h * p.k_sh;
+        u32x4 c[NK];
+        float scale[NK];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int d = ch * 8 + j;
-                x[j] = ldexpf(from_e4m3(codes[is_v ? (size_t)d * page + token : (size_t)token * D + d]), e);
+        for (int x = 0; x < NK; ++x) {
+            const int i = x * kThreads + tid, s = s0 + i / CPR;
+            const long long pos = (long long)p.first + s;
+            const int at = s < p.S ? lookup(pos) : -1;
+            c[x] = u32x4{0, 0, 0, 0};
+            scale[x] = 1.f;
+            if (at >= 0) {
+                const size_t unit = (size_t)at * p.c.Hkv + h;
+                c[x] = *(const u32x4*)(p.c.k + (unit * page + (pos & (page - 1))) * D + 16 * (i % CPR));
+                scale[x] = __uint_as_float((unsigned)p.c.ke[unit] << 23);
             }
+        }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(x[2 * j], x[2 * j + 1]);
+        for (int x = 0; x < NK; ++x) {
+            const int i = x * kThreads + tid, s = s0 + i / CPR;
+            unsigned w[8];
+            decode16(c[x], scale[x], w);
+            if (s < p.S) {
+                u32x4* const o = (u32x4*)(out + s * p.k_ss + 16 * (i % CPR));
+                o[0] = u32x4{w[0], w[1], w[2], w[3]};
+                o[1] = u32x4{w[4], w[5], w[6], w[7]};
+            }
+        }
+    } else {
+        if (p.first % 16 == 0) {
+            if (tid < 2 * D) {
+                const int g = tid & 3, d = tid >> 2 << 1;              // (groups side by side: 64 consecutive codes of a column)
+                const long long pos = (long long)p.first + s0 + 16 * g;
+                const int at = lookup(pos);
+                u32x4 c[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+                float scale = 1.f;
+                if (at >= 0) {
+                    const size_t unit = (size_t)at * p.c.Hkv + h;
+                    const unsigned char* const v = p.c.v + unit * page * D + (pos & (page - 1));
+                    c[0] = *(const u32x4*)(v + d * page);
+                    c[1] = *(const u32x4*)(v + d * page + page);
+                    scale = __uint_as_float((unsigned)p.c.ve[unit] << 23);
+                }
+                unsigned w0[8], w1[8];
+                decode16(c[0], scale, w0);
+                decode16(c[1], scale, w1);
+                const int left = (int)min((long long)n - pos, 16LL);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const unsigned s = 16 * (j % 2), pair = (w0[j / 2] >> s & 0xffff) | (w1[j / 2] >> s) << 16;
+                    s_rows[(16 * g + j) * (D / 2) + (d / 2 ^ (16 * g & (D / 2 - 1)))] = j < left ? pair : 0u;
+                }
+            }
+        } else {
+            // a start inside a group of 16: code by code
+            for (int i = tid; i < kReadRows * D / 2; i += kThreads) {
+                const int t = i % kReadRows, d = i / kReadRows * 2;
+                const long long pos = (long long)p.first + s0 + t;
+                const int at = lookup(pos);
+                unsigned pair = 0;
+                if (at >= 0) {
+                    const size_t unit = (size_t)at * p.c.Hkv + h;
+                    const unsigned char* const v = p.c.v + unit * page * D + d * page + (pos & (page - 1));
+                    pair = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)v[0] | (unsigned)v[page] << 8,
+                                                                                                __uint_as_float((unsigned)p.c.ve[unit] << 23), false));
+                }
+                s_rows[t * (D / 2) + (d / 2 ^ (16 * (t / 16) & (D / 2 - 1)))] = pair;
+            }
+        }
+        __syncthreads();
+        __bf16* const out = p.v + b * p.v_sb + h * p.v_sh;
+        for (int i = tid; i < kReadRows * (D / 8); i += kThreads) {
+            const int t = i / (D / 8), c = i % (D / 8);
+            if (s0 + t < p.S) *(u32x4*)(out + (s0 + t) * p.v_ss + 8 * c) = *(const u32x4*)&s_rows[t * (D / 2) + 4 * (c ^ (4 * (t / 16) & (D / 8 - 1)))];
         }
     }
-    __bf16* const out = is_v ? p.v + b * p.v_sb + h * p.v_sh + s * p.v_ss : p.k + b * p.k_sb + h * p.k_sh + s * p.k_ss;
-    *(u32x4*)(out + ch * 8) = w;
 }
 
 }  // namespace
 
+template <int PAGE>
+static void launch_write(const KvWriteParams& p, dim3 grid, hipStream_t stream) {
+    if (p.c.D == 128) hipLaunchKernelGGL((kv_write<128, PAGE>), grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((kv_write<64, PAGE>), grid, dim3(kThreads), 0, stream, p);
+}
+
 int kv_write_launch(const KvWriteParams& p, hipStream_t stream) {
-    const double blocks = (double)p.B * p.F * p.c.Hkv;
+    const double units = (double)p.B * p.F * p.c.Hkv;
+    const int per = p.c.page <= 32 ? 4 : 1;
+    const double blocks = (units + per - 1) / per;
     if (blocks * kThreads >= 4294967296.0) return -2;
     const dim3 grid((unsigned)blocks, 2);
-    if (p.c.D == 128) hipLaunchKernelGGL(kv_write<128>, grid, dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL(kv_write<64>, grid, dim3(kThreads), 0, stream, p);
+    if (p.c.page == 16) launch_write<16>(p, grid, stream);
+    else if (p.c.page == 32) launch_write<32>(p, grid, stream);
+    else if (p.c.page == 64) launch_write<64>(p, grid, stream);
+    else launch_write<128>(p, grid, stream);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 
 int kv_read_launch(const KvReadParams& p, hipStream_t stream) {
-    const double threads = (double)p.B * p.c.Hkv * p.S * (p.c.D / 8);
-    if (threads >= 4294967296.0 - kThreads) return -2;
-    const dim3 grid((unsigned)((threads + kThreads - 1) / kThreads), 2);
+    const double blocks = (double)p.B * p.c.Hkv * ((p.S + kReadRows - 1) / kReadRows);
+    if (blocks * kThreads >= 4294967296.0) return -2;
+    const dim3 grid((unsigned)blocks, 2);
     if (p.c.D == 128) hipLaunchKernelGGL(kv_read<128>, grid, dim3(kThreads), 0, stream, p);
     else hipLaunchKernelGGL(kv_read<64>, grid, dim3(kThreads), 0, stream, p);
     return hipGetLastError() == hipSuccess ? 0 : -1;

@@ -14,6 +14,7 @@ namespace {
 using namespace gfx950;
 
 constexpr int kThreads = 256;
+constexpr double kFull = 1 << 19;
 
 template <int N> struct Chunk;                          // N bf16 values as one access
 template <> struct Chunk<8> { using type = u32x4; };
@@ -69,6 +70,7 @@ __global__ __launch_bounds__(kThreads) void rope_turn(RopeParams p) {
         c[i] *= p.mscale;
         sn[i] *= p.mscale * p.sign;
     }
+#pragma unroll 4
     for (int h = h0; h < h1; ++h, in += t.in_sh, out += t.out_sh) {
         if constexpr (IL) {
             float x[2 * V], y[2 * V];
@@ -99,7 +101,10 @@ void launch(RopeParams p, hipStream_t stream) {
     const bool in_place = p.t[0].in == p.t[0].out && (p.t[1].heads == 0 || p.t[1].in == p.t[1].out);
     p.items = p.R / 2 / V + (in_place ? 0 : (p.D - p.R) / (IL ? 2 * V : V));
     const long long tokens = (long long)p.B * p.S;
-    p.per = 1;
+    // heads per thread: as many as leave the chip kFull threads
+    const double threads = (double)tokens * p.items * (p.t[0].heads + p.t[1].heads);
+    const int most = p.t[0].heads > p.t[1].heads ? p.t[0].heads : p.t[1].heads;
+    p.per = threads < 2 * kFull ? 1 : threads / kFull < most ? (int)(threads / kFull) : most;
     p.chunks_q = (p.t[0].heads + p.per - 1) / p.per;
     const unsigned rows = p.chunks_q + (p.t[1].heads + p.per - 1) / p.per;
     const unsigned blocks = (unsigned)((tokens * p.items + kThreads - 1) / kThreads);
