@@ -23,7 +23,6 @@ namespace {
 using namespace gfx950;
 
 constexpr int kTile = 64;            // keys per tile
-constexpr int kWaves = 4;
 constexpr int kBlock = 16;           // packed query rows per block
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -47,6 +46,20 @@ __device__ __forceinline__ Seen seen_tiles(const KvAttnParams& p, int b, int g, 
     return s;
 }
 
+// Tiles of a part.  All sequences' parts have one size, by the longest of them: the workgroups of a batch with caches of all
+// lengths then take equally long.  (Never so few that a sequence had more parts than there is room for.)
+__device__ __forceinline__ int part_tiles(const KvAttnParams& p, const Seen& seen, int lane) {
+    if (p.splits == 1) return seen.count;
+    int longest = seen.n;
+    if (p.B > 1) {
+        for (int x = lane; x < p.B; x += 64) longest = max(longest, p.lens[x]);
+#pragma unroll
+        for (int x = 32; x > 0; x >>= 1) longest = max(longest, __shfl_xor(longest, x));
+    }
+    const int tiles = max(min((min(__builtin_amdgcn_readfirstlane(longest), p.max_len) + kTile - 1) / kTile, p.most_tiles), seen.count);
+    return (tiles + p.splits - 1) / p.splits;
+}
+
 // The largest or the sum over the four lane groups that share a column.
 __device__ __forceinline__ float max_over_groups(float x) { x = fmaxf(x, __shfl_xor(x, 16)); return fmaxf(x, __shfl_xor(x, 32)); }
 __device__ __forceinline__ float sum_over_groups(float x) { x += __shfl_xor(x, 16); return x + __shfl_xor(x, 32); }
@@ -60,18 +73,26 @@ __device__ __forceinline__ bf16x8 decode(unsigned lo, unsigned hi, float scale) 
 // The bytes of w that are the NaN code, as 0x80 each.
 __device__ __forceinline__ unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
+// A part without keys: its rows' maxima say so, its O stays unwritten.
+template <int ROWS>
+__device__ __forceinline__ void no_part(const KvAttnParams& p, int b, int hk, int g, int first, int split) {
+    const int row = first + (int)threadIdx.x, i = row / g, h = row - i * g;
+    if (threadIdx.x < ROWS && i < p.Sq)
+        *(f32x2*)(p.ml + 2 * ((((size_t)b * p.Hq + hk * g + h) * p.Sq + i) * p.splits + split)) = f32x2{-INFINITY, 0.f};
+}
+
 template <int D> constexpr int merge_pitch() { return D + 4; }      // floats per O row in the merge area
 
 // NR blocks of 16 packed rows per workgroup, every wavefront all of them.
-template <int D, int NR>
-__global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
+template <int D, int NR, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
     constexpr int KC = D / 64;                 // 16-byte loads per key and lane
     constexpr int DT = D / 16;                 // 16-row blocks of O^T
     constexpr int PITCH = merge_pitch<D>();
     constexpr int ROWS = NR * kBlock;
 
-    __shared__ __attribute__((aligned(16))) float s_o[kWaves * ROWS * PITCH];
-    __shared__ float s_ml[2][kWaves][ROWS];
+    __shared__ __attribute__((aligned(16))) float s_o[NW * ROWS * PITCH];
+    __shared__ float s_ml[2][NW][ROWS];
     __shared__ float s_inv[ROWS];
 
     const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, grp = lane >> 4;
@@ -87,9 +108,10 @@ __global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
 
     const int g = p.Hq / p.c.Hkv, R = g * p.Sq, first = rowblk * ROWS;
     const Seen seen = seen_tiles(p, b, g, first, ROWS);
-    const int per = (seen.count + p.splits - 1) / p.splits;
+    const int per = part_tiles(p, seen, lane);
     const int t0 = split * per, t1 = min(seen.count, t0 + per);
-    if (p.splits > 1 && t0 >= t1) return;                    // attn_kv_combine knows
+    const bool alone = p.splits == 1;                        // the result itself, no part of it
+    if (!alone && t0 >= t1) { no_part<ROWS>(p, b, hk, g, first, split); return; }
 
     // this lane's rows: what they see, and Q.  Rows past the last one see what the last one does and are not stored.
     int hi[NR], lo[NR];
@@ -102,7 +124,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
         hi[r] = p.causal ? min(pos, seen.n - 1) : seen.n - 1;
         lo[r] = p.window ? (int)max((long long)pos - p.window + 1, 0LL) : 0;
         hi_all = max(hi_all, hi[r]); lo_all = min(lo_all, lo[r]);
-        const __bf16* const q = p.q + b * p.q_sb + (hk * g + h) * p.q_sh + (long long)i * p.q_ss;
+        const __bf16* const q = p.q + b * p.q_sb + (hk * g + h) * p.q_sh + (long long)(row / g) * p.q_ss;      // (not i: no wait for the lengths)
 #pragma unroll
         for (int c = 0; c < KC; ++c)
 #pragma unroll
@@ -121,79 +143,91 @@ __global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
     }
     const float c = p.scale_log2;
     const int page = p.c.page, sub_k = col >> 2, key_k = col & 3;
+    const int* const table = p.c.table + b * p.c.pitch;
+    bool poisoned = false;                                   // NaN codes were met where only some rows see them
 
-    // The page of 16 keys, -1 where there is none.
-    auto lookup = [&](int key) __attribute__((always_inline)) {
-        int at = -1;
-        if (key < seen.n) at = p.c.table[b * p.c.pitch + (key >> p.c.page_log2)];
-        return at >= 0 && at < p.c.P ? at : -1;
-    };
     auto tile_of = [&](int t) __attribute__((always_inline)) { return t < seen.sink_tiles ? t : t - seen.sink_tiles + seen.first; };
-
-    for (int t = t0 + wave; t < t1; t += kWaves) {
+    // the pages of this lane's keys in a tile, for K and for V: -1 where there is none
+    struct Pages { int k, v; };
+    auto lookup = [&](int key) __attribute__((always_inline)) {
+        const int at = table[min(key, seen.n - 1) >> p.c.page_log2];           // (no branch around the load: several are in flight)
+        return (int)(key < seen.n) & (int)((unsigned)at < (unsigned)p.c.P) ? at : -1;
+    };
+    auto find = [&](int t) __attribute__((always_inline)) {
         const int key0 = tile_of(t) * kTile;
-        const int at_k = lookup(key0 + 16 * sub_k), at_v = lookup(key0 + 16 * grp);
-        const size_t unit_k = (size_t)max(at_k, 0) * p.c.Hkv + hk, unit_v = (size_t)max(at_v, 0) * p.c.Hkv + hk;
-        const float scale_k = __uint_as_float((unsigned)p.c.ke[unit_k] << 23), scale_v = __uint_as_float((unsigned)p.c.ve[unit_v] << 23);
-        const unsigned char* const kp = p.c.k + unit_k * page * D + (size_t)(((key0 + 16 * sub_k) & (page - 1)) + key_k) * D + 16 * grp;
-        const unsigned char* const vp = p.c.v + unit_v * page * D + col * page + ((key0 + 16 * grp) & (page - 1));
-        u32x4 kr[4][KC], vr[DT];
+        return Pages{lookup(key0 + 16 * sub_k), lookup(key0 + 16 * grp)};
+    };
+    // Loads of a tile's codes.  Behind the last tile every lane reads the cache's first bytes instead: the number of loads in
+    // flight, which the waits count, is the same on every path.
+    u32x4 kr[4][KC], vr[DT];
+    unsigned ke, ve;
+    int at_v;
+    auto load_k = [&](int t, int at) __attribute__((always_inline)) {
+        const size_t unit = (size_t)max(at, 0) * p.c.Hkv + hk;
+        const unsigned char* k = p.c.k + (unit * page + ((tile_of(t) * kTile + 16 * sub_k) & (page - 1)) + key_k) * D + 16 * grp;
+        k = t < t1 ? k : p.c.k;
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-            for (int ch = 0; ch < KC; ++ch) kr[kt][ch] = *(const u32x4*)(kp + 4 * kt * D + 64 * ch);
+            for (int ch = 0; ch < KC; ++ch) kr[kt][ch] = *(const u32x4*)(k + 4 * kt * D + 64 * ch);
+        ke = p.c.ke[unit];
+    };
+    auto load_v = [&](int t, int at) __attribute__((always_inline)) {
+        const size_t unit = (size_t)max(at, 0) * p.c.Hkv + hk;
+        const unsigned char* v = p.c.v + unit * page * D + col * page + ((tile_of(t) * kTile + 16 * grp) & (page - 1));
+        v = t < t1 ? v : p.c.v;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) vr[d] = *(const u32x4*)(vp + d * 16 * page);
-
-        // a tile with keys that some row does not see
-        const int key_g = key0 + 16 * grp;                   // this lane's 16 scores are those of keys key_g ...
+        for (int d = 0; d < DT; ++d) vr[d] = *(const u32x4*)(v + d * 16 * page);
+        ve = p.c.ve[unit];
+        at_v = at;
+    };
+    // which of this lane's 16 keys from `key` on a row sees whose last key is hi and whose window starts at lo
+    auto sees = [&](int key, int hi, int lo, bool there) __attribute__((always_inline)) {
+        auto upto = [](int n) __attribute__((always_inline)) { return (1u << min(max(n, 0), 16)) - 1; };
+        return there ? upto(hi - key + 1) & (~upto(lo - key) | upto(p.sinks - key)) : 0u;
+    };
+    // a tile with keys that some row does not see
+    auto at_edge = [&](int key0, int at_v) __attribute__((always_inline)) {
         bool edge = at_v < 0;
 #pragma unroll
         for (int r = 0; r < NR; ++r) edge = edge || key0 + kTile - 1 > hi[r] || (key0 < lo[r] && key0 + kTile > p.sinks);
-        edge = __builtin_amdgcn_ballot_w64(edge) != 0;
-        bool poisoned = false;
-        if (edge) {
-            // codes that no row sees become zero: the product 0 * NaN must not reach a row
-            u32x4 keep = {0, 0, 0, 0};
+        return __builtin_amdgcn_ballot_w64(edge) != 0;
+    };
+
+    f32x4 sc[NR][4];
+    bf16x8 pf[NR][2];
+    auto scores = [&]() __attribute__((always_inline)) {
+        const float scale = __uint_as_float(ke << 23);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int key = key_g + j;
-                if (at_v >= 0 && key <= hi_all && (key >= lo_all || key < p.sinks)) keep[j / 4] |= 0xffu << (8 * (j % 4));
+        for (int kt = 0; kt < 4; ++kt) {
+#pragma unroll
+            for (int r = 0; r < NR; ++r) sc[r][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ch = 0; ch < KC; ++ch)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const bf16x8 kf = decode(kr[kt][ch][2 * u], kr[kt][ch][2 * u + 1], scale);
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) sc[r][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][2 * ch + u], sc[r][kt], 0, 0, 0);
+                }
+        }
+    };
+    auto softmax = [&](int t) __attribute__((always_inline)) {
+        const int key0 = tile_of(t) * kTile;
+        if (at_edge(key0, at_v)) {
+            const int key = key0 + 16 * grp;                 // this lane's scores are those of 16 keys from here on
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const unsigned visible = sees(key, hi[r], lo[r], at_v >= 0);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sc[r][j / 4][j % 4] = visible >> j & 1 ? sc[r][j / 4][j % 4] : -INFINITY;
             }
-            unsigned bad = 0;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                vr[d] &= keep;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) bad |= nan_codes(vr[d][j]);
-            }
-            poisoned = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
         }
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            f32x4 sc[4];
+            float mx = sc[r][0][0];
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
-                sc[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int ch = 0; ch < KC; ++ch) {
-                    sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(kr[kt][ch][0], kr[kt][ch][1], scale_k), qf[r][2 * ch], sc[kt], 0, 0, 0);
-                    sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(kr[kt][ch][2], kr[kt][ch][3], scale_k), qf[r][2 * ch + 1], sc[kt], 0, 0, 0);
-                }
-            }
-            unsigned visible = 0xffffu;
-            if (edge) {
-                visible = 0;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const int key = key_g + j;
-                    if (at_v >= 0 && key <= hi[r] && (key >= lo[r] || key < p.sinks)) visible |= 1u << j;
-                    else sc[j / 4][j % 4] = -INFINITY;
-                }
-            }
-            float mx = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) mx = fmaxf(mx, sc[j / 4][j % 4]);
+            for (int j = 1; j < 16; ++j) mx = fmaxf(mx, sc[r][j / 4][j % 4]);
             const float m_new = fmaxf(m_run[r], max_over_groups(mx));
             const float m_use = m_new == -INFINITY ? 0.f : m_new;
             const float alpha = exp2_hw((m_run[r] - m_use) * c), mc = m_use * c;
@@ -202,7 +236,7 @@ __global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
             unsigned pk[8];
 #pragma unroll
             for (int j = 0; j < 16; j += 2) {
-                const float p0 = exp2_hw(fmaf(sc[j / 4][j % 4], c, -mc)), p1 = exp2_hw(fmaf(sc[j / 4][j % 4 + 1], c, -mc));
+                const float p0 = exp2_hw(fmaf(sc[r][j / 4][j % 4], c, -mc)), p1 = exp2_hw(fmaf(sc[r][j / 4][j % 4 + 1], c, -mc));
                 sum += p0 + p1;
                 pk[j / 2] = pack_bf16x2(p0, p1);
             }
@@ -210,38 +244,84 @@ __global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
             if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0)
 #pragma unroll
                 for (int d = 0; d < DT; ++d) oacc[r][d] *= alpha;
-            const bf16x8 pf0 = __builtin_bit_cast(bf16x8, (u32x4{pk[0], pk[1], pk[2], pk[3]}));
-            const bf16x8 pf1 = __builtin_bit_cast(bf16x8, (u32x4{pk[4], pk[5], pk[6], pk[7]}));
-            if (!poisoned) {
+            pf[r][0] = __builtin_bit_cast(bf16x8, (u32x4{pk[0], pk[1], pk[2], pk[3]}));
+            pf[r][1] = __builtin_bit_cast(bf16x8, (u32x4{pk[4], pk[5], pk[6], pk[7]}));
+        }
+    };
+    auto weigh = [&](int t) __attribute__((always_inline)) {
+        const int key0 = tile_of(t) * kTile;
+        const float scale = __uint_as_float(ve << 23);
+        if (at_edge(key0, at_v)) {
+            // NaN codes become zero: the probability 0 of a row that does not see them must not meet them
+            const unsigned some = sees(key0 + 16 * grp, hi_all, lo_all, at_v >= 0);
+            unsigned bad = 0;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned nan = nan_codes(vr[d][j]) >> 7;
+                    vr[d][j] &= ~(nan * 0xffu);
+                    bad |= (nan * 0x10204080u >> 28) << (4 * j);                      // bytes 0 ... 3 to bits 0 ... 3
+                }
+            poisoned = poisoned || __builtin_amdgcn_ballot_w64((bad & some) != 0) != 0;
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const bf16x8 vf = decode(vr[d][2 * u], vr[d][2 * u + 1], scale);
+#pragma unroll
+                for (int r = 0; r < NR; ++r) oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][u], oacc[r][d], 0, 0, 0);
+            }
+    };
+
+    // A tile's K is on its way while the one before it is weighed, its V while its scores are made; its pages are looked up a tile
+    // earlier still, and asked for before the codes of the tile in between (loads return in order).
+    int t = t0 + wave;
+    if (t < t1) {
+        const Pages now = find(t);
+        Pages at = find(min(t + NW, t1 - 1));
+        load_k(t, now.k);
+        load_v(t, now.v);
+        for (; t < t1; t += NW) {
+            const Pages then = find(min(t + 2 * NW, t1 - 1));
+            scores();
+            __builtin_amdgcn_sched_barrier(0);
+            load_k(t + NW, at.k);
+            __builtin_amdgcn_sched_barrier(0);
+            softmax(t);
+            weigh(t);
+            __builtin_amdgcn_sched_barrier(0);
+            load_v(t + NW, at.v);
+            at = then;
+        }
+    }
+    if (poisoned) {
+        // once more through the tiles at an edge: a NaN for every row that sees a NaN code, in that code's column
+        for (t = t0 + wave; t < t1; t += NW) {
+            const int key0 = tile_of(t) * kTile, key = key0 + 16 * grp;
+            load_v(t, lookup(key));
+            if (!at_edge(key0, at_v)) continue;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const unsigned visible = sees(key, hi[r], lo[r], at_v >= 0);
+                u32x4 see[2];
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    see[j / 4][j % 4] = (visible >> (2 * j) & 1) * 0x3f80u | (visible >> (2 * j + 1) & 1) * 0x3f800000u;     // ones in bf16
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(vr[d][0], vr[d][1], scale_v), pf0, oacc[r][d], 0, 0, 0);
-                    oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(vr[d][2], vr[d][3], scale_v), pf1, oacc[r][d], 0, 0, 0);
-                }
-            } else {
-                // NaN codes among keys that only some rows see: without them, and then a NaN for every row that sees one
-                bf16x8 see0, see1;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    see0[j] = (__bf16)((visible >> j) & 1 ? 1.f : 0.f);
-                    see1[j] = (__bf16)((visible >> (8 + j)) & 1 ? 1.f : 0.f);
-                }
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    bf16x8 ind[2];
-                    u32x4 w = vr[d];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const unsigned nan = nan_codes(w[j]);
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) ind[j / 2][4 * (j % 2) + y] = (__bf16)((nan >> (8 * y + 7)) & 1 ? 1.f : 0.f);
-                        w[j] &= ~((nan >> 7) * 0xffu);
-                    }
                     f32x4 hits = {0.f, 0.f, 0.f, 0.f};
-                    hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ind[0], see0, hits, 0, 0, 0);
-                    hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ind[1], see1, hits, 0, 0, 0);
-                    oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(w[0], w[1], scale_v), pf0, oacc[r][d], 0, 0, 0);
-                    oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode(w[2], w[3], scale_v), pf1, oacc[r][d], 0, 0, 0);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        u32x4 ind;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const unsigned nan = nan_codes(vr[d][2 * u + j / 2]) >> (16 * (j % 2) + 7);
+                            ind[j] = (nan & 1) * 0x3f80u | (nan >> 8 & 1) * 0x3f800000u;
+                        }
+                        hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ind), __builtin_bit_cast(bf16x8, see[u]), hits, 0, 0, 0);
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) oacc[r][d][e] = hits[e] > 0.f ? NAN : oacc[r][d][e];
                 }
@@ -261,22 +341,23 @@ __global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
         const int row = r * kBlock + col;
         float m = s_ml[0][0][row];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_ml[0][w][row]);
+        for (int w = 1; w < NW; ++w) m = fmaxf(m, s_ml[0][w][row]);
         const float f = m_run[r] == -INFINITY ? 0.f : exp2_hw((m_run[r] - m) * c);
+        if (first + row < R)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *(f32x4*)(s_o + (wave * ROWS + row) * PITCH + 16 * d + 4 * grp) = oacc[r][d] * f;
+            for (int d = 0; d < DT; ++d) *(f32x4*)(s_o + (wave * ROWS + row) * PITCH + 16 * d + 4 * grp) = oacc[r][d] * f;
     }
     if (tid < ROWS && first + tid < R) {
         const int row = first + tid, i = row / g, h = row - i * g;
         const size_t rowi = ((size_t)b * p.Hq + hk * g + h) * p.Sq + i;
         float m = s_ml[0][0][tid], l = 0.f;
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_ml[0][w][tid]);
+        for (int w = 1; w < NW; ++w) m = fmaxf(m, s_ml[0][w][tid]);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) l += s_ml[1][w][tid] * (s_ml[0][w][tid] == -INFINITY ? 0.f : exp2_hw((s_ml[0][w][tid] - m) * c));
+        for (int w = 0; w < NW; ++w) l += s_ml[1][w][tid] * (s_ml[0][w][tid] == -INFINITY ? 0.f : exp2_hw((s_ml[0][w][tid] - m) * c));
         const bool none = l == 0.f || i >= seen.rows;
         s_inv[tid] = none ? 0.f : 1.f / l;
-        if (p.splits == 1) {
+        if (alone) {
             if (p.lse) p.lse[rowi] = none ? -INFINITY : m * p.scale + logf(l);
         } else {
             *(f32x2*)(p.ml + 2 * (rowi * p.splits + split)) = f32x2{none ? -INFINITY : m, none ? 0.f : l};
@@ -284,14 +365,14 @@ __global__ __launch_bounds__(kWaves * 64) void attn_kv_rows(KvAttnParams p) {
     }
     __syncthreads();
     constexpr int QPR = D / 4;
-    for (int item = tid; item < ROWS * QPR; item += kWaves * 64) {
+    for (int item = tid; item < ROWS * QPR; item += NW * 64) {
         const int rr = item / QPR, d = item % QPR * 4, row = first + rr;
         if (row >= R) break;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += *(const f32x4*)(s_o + (w * ROWS + rr) * PITCH + d);
+        for (int w = 0; w < NW; ++w) v += *(const f32x4*)(s_o + (w * ROWS + rr) * PITCH + d);
         const int i = row / g, h = row - i * g;
-        if (p.splits == 1) {
+        if (alone) {
             const float inv = s_inv[rr];
             u32x2 w2 = {0, 0};
             if (inv != 0.f) w2 = u32x2{pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv)};
@@ -341,9 +422,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
 
     const int g = p.Hq / p.c.Hkv, R = g * p.Sq, first = rowblk * ROWS;
     const Seen seen = seen_tiles(p, b, g, first, ROWS);
-    const int per = (seen.count + p.splits - 1) / p.splits;
+    const int per = part_tiles(p, seen, lane);
     const int t0 = split * per, t1 = min(seen.count, t0 + per);
-    if (p.splits > 1 && t0 >= t1) return;
+    const bool alone = p.splits == 1;                     // the result itself, no part of it
+    if (!alone && t0 >= t1) { no_part<ROWS>(p, b, hk, g, first, split); return; }
 
     // this lane's row; rows past the last one see what it does and are not stored
     const int row = min(first + wave * kTileRows + (lane & 31), R - 1), row_i = row / g, hq = hk * g + row - row_i * g;
@@ -589,7 +671,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
     if (r >= R) return;
     const size_t rowi = ((size_t)b * p.Hq + hq) * p.Sq + row_i;
     const bool none = l == 0.f || row_i >= seen.rows;
-    if (p.splits == 1) {
+    if (alone) {
         const float inv = none ? 0.f : 1.f / l;
         __bf16* const o = p.o + b * p.o_sb + hq * p.o_sh + (long long)row_i * p.o_ss;
 #pragma unroll
@@ -610,36 +692,58 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
     }
 }
 
-// O and LSE of a row from the parts of its splits: one workgroup per row.
+// O and LSE of a row from the parts of its splits: one workgroup per row, D / 4 threads for a part, its loads in batches of NL in
+// flight per thread (the parts come from L2 or the memory-side cache: latency counts).
 template <int D>
-__global__ __launch_bounds__(256) void attn_kv_combine(KvAttnParams p, int rows_per_wg) {
-    constexpr int QPR = D / 4, NS = 256 / QPR;
-    __shared__ float s_w[kMaxKvSplits];
+__global__ __launch_bounds__(256) void attn_kv_combine(KvAttnParams p) {
+    constexpr int QPR = D / 4, NS = 256 / QPR, NL = 8, NM = kMaxKvSplits / 64;
     __shared__ float s_red[NS][D];
-    const int tid = threadIdx.x, lane = tid & 63, g = p.Hq / p.c.Hkv;
-    const size_t rowi = blockIdx.x;
-    const int i = (int)(rowi % p.Sq), hq = (int)(rowi / p.Sq % p.Hq), b = (int)(rowi / p.Sq / p.Hq);
-    const int row = i * g + hq % g;
-    const Seen seen = seen_tiles(p, b, g, row / rows_per_wg * rows_per_wg, rows_per_wg);
-    const int per = (seen.count + p.splits - 1) / p.splits;
-    const int S = per > 0 && i < seen.rows ? (seen.count + per - 1) / per : 0;     // splits that left a part
-    float m = -INFINITY, l = 0.f;
-    for (int s = lane; s < S; s += 64) m = fmaxf(m, p.ml[2 * (rowi * p.splits + s)]);
+    const int tid = threadIdx.x, lane = tid & 63, sl = tid / QPR, d = tid % QPR * 4, S = p.splits;
+    const unsigned rowi = blockIdx.x, bh = rowi / (unsigned)p.Sq;
+    const int i = rowi - bh * p.Sq, b = bh / (unsigned)p.Hq, hq = bh - b * p.Hq;
+    const float* const part = p.part + (size_t)rowi * S * D + d;
+    const float* const ml = p.ml + 2 * ((size_t)rowi * S);
+    f32x4 v[NL];
+    auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < NL; ++n) {
+            const int s = s0 + sl + n * NS;
+            v[n] = s < S ? *(const f32x4*)(part + (size_t)s * D) : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    // the parts' weights: of part 64 j + lane in w[j]
+    float mm[NM], ll[NM], w[NM], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int j = 0; j < NM; ++j) {
+        const int s = 64 * j + lane;
+        const f32x2 x = s < S ? *(const f32x2*)(ml + 2 * s) : f32x2{-INFINITY, 0.f};
+        mm[j] = x[0]; ll[j] = x[1];
+    }
+    load(0);
+#pragma unroll
+    for (int j = 0; j < NM; ++j) m = fmaxf(m, mm[j]);
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-    for (int s = lane; s < S; s += 64) {
-        const f32x2 ml = *(const f32x2*)(p.ml + 2 * (rowi * p.splits + s));
-        const float w = ml[0] == -INFINITY ? 0.f : exp2_hw((ml[0] - m) * p.scale_log2);
-        l += ml[1] * w;
-        if (tid < 64) s_w[s] = w;
+#pragma unroll
+    for (int j = 0; j < NM; ++j) {
+        w[j] = mm[j] == -INFINITY ? 0.f : exp2_hw((mm[j] - m) * p.scale_log2);
+        l += ll[j] * w[j];
     }
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x);
-    __syncthreads();
-    const int sl = tid / QPR, d = tid % QPR * 4;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s = sl; s < S; s += NS)
-        acc += *(const f32x4*)(p.part + (rowi * p.splits + s) * D + d) * s_w[s];
+#pragma unroll
+    for (int j = 0; j < kMaxKvSplits / (NL * NS); ++j) {
+        if (j * NL * NS < S) {
+            if (j > 0) load(j * NL * NS);
+#pragma unroll
+            for (int n = 0; n < NL; ++n) {
+                const int s = j * NL * NS + n * NS + sl;                              // (its weight's register does not depend on sl)
+                const float ws = __shfl(w[(j * NL * NS + n * NS) / 64], s & 63), ms = __shfl(mm[(j * NL * NS + n * NS) / 64], s & 63);
+                if (ms != -INFINITY) acc += v[n] * ws;                                // (a part without keys is not written)
+            }
+        }
+    }
     *(f32x4*)&s_red[sl][d] = acc;
     __syncthreads();
     if (tid < D / 2) {
@@ -655,33 +759,36 @@ __global__ __launch_bounds__(256) void attn_kv_combine(KvAttnParams p, int rows_
 
 }  // namespace
 
-constexpr int tile_waves(int D) { return D == 128 ? 4 : 4; }
-
 // Rows per workgroup: 16 where that is all there is, else 32 rows per wavefront that share decoded tiles.
 KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits) {
     KvAttnPlan plan;
     const long long R = (long long)(Hq / Hkv) * Sq;
-    plan.rows = R <= kBlock ? kBlock : tile_waves(D) * kTileRows;
+    plan.rows = R <= kBlock ? kBlock : 4 * kTileRows;
+    plan.waves = plan.rows == kBlock && (long long)B * Hkv < 512 ? 8 : 4;
     plan.row_wgs = (int)((R + plan.rows - 1) / plan.rows);
     plan.splits = splits;
+    plan.keys = keys;
     if (splits == 0) {
-        const int tiles = (keys + kTile - 1) / kTile, most = plan.rows == kBlock ? (tiles + kWaves - 1) / kWaves : (tiles + 3) / 4;
+        const int tiles = (keys + kTile - 1) / kTile, most = plan.rows == kBlock ? (tiles + plan.waves - 1) / plan.waves : (tiles + 3) / 4;
         const long long base = (long long)B * Hkv * plan.row_wgs;
-        long long s = (plan.rows == kBlock ? 1024 : 512) / base;
+        long long s = (plan.rows == kBlock ? 512 : 512) / base;
         if (s > most) s = most;
         plan.splits = s < 1 ? 1 : s > kMaxKvSplits ? kMaxKvSplits : (int)s;
     }
+    (void)D;
     return plan;
 }
 
 template <int D>
 static void launch(const KvAttnParams& p, const KvAttnPlan& plan, unsigned blocks, hipStream_t stream) {
-    if (plan.rows == kBlock) hipLaunchKernelGGL((attn_kv_rows<D, 1>), dim3(blocks), dim3(kWaves * 64), 0, stream, p);
-    else hipLaunchKernelGGL((attn_kv_tiles<D, tile_waves(D)>), dim3(blocks), dim3(tile_waves(D) * 64), 0, stream, p);
+    if (plan.rows == kBlock && plan.waves == 8) hipLaunchKernelGGL((attn_kv_rows<D, 1, 8>), dim3(blocks), dim3(512), 0, stream, p);
+    else if (plan.rows == kBlock) hipLaunchKernelGGL((attn_kv_rows<D, 1, 4>), dim3(blocks), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL((attn_kv_tiles<D, 4>), dim3(blocks), dim3(256), 0, stream, p);
 }
 
 int attn_kv_launch(KvAttnParams p, const KvAttnPlan& plan, hipStream_t stream) {
     p.row_wgs = plan.row_wgs; p.splits = plan.splits;
+    p.most_tiles = (plan.keys + kTile - 1) / kTile;
     const double blocks = (double)p.B * p.c.Hkv * p.row_wgs * p.splits;
     if (blocks * 512 >= 4294967296.0) return -2;
     if (p.c.D == 128) launch<128>(p, plan, (unsigned)blocks, stream);
@@ -689,8 +796,8 @@ int attn_kv_launch(KvAttnParams p, const KvAttnPlan& plan, hipStream_t stream) {
     if (hipGetLastError() != hipSuccess) return -1;
     if (p.splits > 1) {
         const unsigned rows = (unsigned)p.B * p.Hq * p.Sq;
-        if (p.c.D == 128) hipLaunchKernelGGL(attn_kv_combine<128>, dim3(rows), dim3(256), 0, stream, p, plan.rows);
-        else hipLaunchKernelGGL(attn_kv_combine<64>, dim3(rows), dim3(256), 0, stream, p, plan.rows);
+        if (p.c.D == 128) hipLaunchKernelGGL(attn_kv_combine<128>, dim3(rows), dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL(attn_kv_combine<64>, dim3(rows), dim3(256), 0, stream, p);
         if (hipGetLastError() != hipSuccess) return -1;
     }
     return 0;

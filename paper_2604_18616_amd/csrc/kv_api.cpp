@@ -69,10 +69,10 @@ extern "C" int kv_fp8_read(const KvFp8Cache* cache, const int* table, long long 
     return answer(kv_read_launch(p, (hipStream_t)stream));
 }
 
-// Keys that the rows of a workgroup see at the most, for dividing the work.
+// Keys in the tiles of 64 that the rows of a workgroup see at the most: a window's and the first tokens' tiles begin and end anywhere.
 static int keys_seen(int Sq, int max_len, int window, int sinks) {
     if (!window) return max_len;
-    const long long keys = (long long)window + (sinks < max_len ? sinks : max_len) + Sq + 128;
+    const long long keys = (long long)window + (sinks < max_len ? sinks : max_len) + Sq + 192;
     return keys < max_len ? (int)keys : max_len;
 }
 

@@ -40,6 +40,7 @@ struct KvAttnParams {
     int causal, window, sinks;
     float scale, scale_log2;
     int row_wgs, splits;           // workgroups along the packed query rows of a kv head, and along its keys
+    int most_tiles;                // that the rows of a workgroup can see
     float *part, *ml;              // [B*Hq*Sq, splits, D] and [B*Hq*Sq, splits, 2], as in attn_launch.h
 };
 
@@ -49,6 +50,6 @@ int kv_read_launch(const KvReadParams& p, hipStream_t stream);
 
 // How a call's rows and keys are cut; splits 0: by size.  Host arithmetic only.
 constexpr int kMaxKvSplits = 256;
-struct KvAttnPlan { int rows, row_wgs, splits; };       // rows: packed query rows per workgroup
+struct KvAttnPlan { int rows, waves, row_wgs, splits, keys; };       // rows: packed query rows per workgroup; keys: that they can see
 KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits);
 int attn_kv_launch(KvAttnParams p, const KvAttnPlan& plan, hipStream_t stream);
