@@ -548,7 +548,8 @@ def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=Fal
     ws = _scratch(need, device) if need else None
     with _on(device):
         rc = lib.attn_kv_fp8(q.data_ptr(), ctypes.byref(struct), at, pitch, width, lens, q_lens, o.data_ptr(), lse.data_ptr(), B, Hq, Sq, qs, os_,
-                             1 if causal else 0, window, sinks, scale, max_len, None if ws is None else ws.data_ptr(), need if ws is not None else 0, 0, stream)
+                             1 if causal else 0, window, sinks, scale, max_len, None if ws is None else ws.data_ptr(), 0 if ws is None else need,
+                             1 if ws is None else need // (4 * B * Hq * Sq * (D + 2)), stream)
     if rc != 0:
         raise AttnError(rc, strerror(rc))
     return o, lse

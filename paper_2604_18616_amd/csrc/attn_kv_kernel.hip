@@ -13,6 +13,8 @@
 // The keys are cut over the wavefronts of a workgroup and over `splits` workgroups; the wavefronts are merged through LDS,
 // the workgroups of a row by attn_kv_combine from fp32 parts.
 #include <hip/hip_runtime.h>
+#include <limits.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "gfx950_prims.h"
@@ -24,6 +26,11 @@ using namespace gfx950;
 
 constexpr int kTile = 64;            // keys per tile
 constexpr int kBlock = 16;           // packed query rows per block
+// The reference that scores are taken relative to is a maximum that a row had once: it is made anew only where a score exceeds it
+// by more than this, as a power of two of the probability.  Neither fp32 sums nor bf16 probabilities lose anything by such a
+// factor, and a tile is spared the exchange of its maximum between lanes and the rescaling.
+constexpr float kSlack = 10.f;
+__device__ __forceinline__ float finite(float m) { return m == -INFINITY ? 0.f : m; }      // (the reference of a row that has seen nothing)
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -83,13 +90,13 @@ __device__ __forceinline__ void no_part(const KvAttnParams& p, int b, int hk, in
 
 template <int D> constexpr int merge_pitch() { return D + 4; }      // floats per O row in the merge area
 
-// NR blocks of 16 packed rows per workgroup, every wavefront all of them.
-template <int D, int NR, int NW>
+// One block of packed rows per workgroup, every wavefront all of it.
+template <int D, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
     constexpr int KC = D / 64;                 // 16-byte loads per key and lane
     constexpr int DT = D / 16;                 // 16-row blocks of O^T
     constexpr int PITCH = merge_pitch<D>();
-    constexpr int ROWS = NR * kBlock;
+    constexpr int ROWS = kBlock;
 
     __shared__ __attribute__((aligned(16))) float s_o[NW * ROWS * PITCH];
     __shared__ float s_ml[2][NW][ROWS];
@@ -113,35 +120,26 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
     const bool alone = p.splits == 1;                        // the result itself, no part of it
     if (!alone && t0 >= t1) { no_part<ROWS>(p, b, hk, g, first, split); return; }
 
-    // this lane's rows: what they see, and Q.  Rows past the last one see what the last one does and are not stored.
-    int hi[NR], lo[NR];
-    bf16x8 qf[NR][KC * 2];
-    int hi_all = -1, lo_all = INT_MAX;                       // what any row of the workgroup sees
+    // this lane's row: what it sees, and Q.  Rows past the last one see what the last one does and are not stored.
+    bf16x8 qf[KC * 2];
+    const int row = min(first + col, R - 1), i = min(row / g, max(seen.rows - 1, 0)), h = row - row / g * g;
+    const int pos = seen.pos0 + i;
+    const int hi = p.causal ? min(pos, seen.n - 1) : seen.n - 1;
+    const int lo = p.window ? (int)max((long long)pos - p.window + 1, 0LL) : 0;
+    int hi_all = hi, lo_all = lo;                            // what any row of the workgroup sees
+    const __bf16* const q = p.q + b * p.q_sb + (hk * g + h) * p.q_sh + (long long)(row / g) * p.q_ss;      // (not i: no wait for the lengths)
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        const int row = min(first + r * kBlock + col, R - 1), i = min(row / g, max(seen.rows - 1, 0)), h = row - row / g * g;
-        const int pos = seen.pos0 + i;
-        hi[r] = p.causal ? min(pos, seen.n - 1) : seen.n - 1;
-        lo[r] = p.window ? (int)max((long long)pos - p.window + 1, 0LL) : 0;
-        hi_all = max(hi_all, hi[r]); lo_all = min(lo_all, lo[r]);
-        const __bf16* const q = p.q + b * p.q_sb + (hk * g + h) * p.q_sh + (long long)(row / g) * p.q_ss;      // (not i: no wait for the lengths)
+    for (int c = 0; c < KC; ++c)
 #pragma unroll
-        for (int c = 0; c < KC; ++c)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) qf[r][2 * c + u] = *(const bf16x8*)(q + (grp + 4 * c) * 16 + 8 * u);
-    }
+        for (int u = 0; u < 2; ++u) qf[2 * c + u] = *(const bf16x8*)(q + (grp + 4 * c) * 16 + 8 * u);
 #pragma unroll
     for (int x = 1; x < 16; x <<= 1) { hi_all = max(hi_all, __shfl_xor(hi_all, x)); lo_all = min(lo_all, __shfl_xor(lo_all, x)); }
 
-    f32x4 oacc[NR][DT];
-    float m_run[NR], l_run[NR];
+    f32x4 oacc[DT];
+    float m_run = -INFINITY, l_run = 0.f;
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        m_run[r] = -INFINITY; l_run[r] = 0.f;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) oacc[r][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    const float c = p.scale_log2;
+    for (int d = 0; d < DT; ++d) oacc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float c = p.scale_log2, slack = kSlack / c;
     const int page = p.c.page, sub_k = col >> 2, key_k = col & 3;
     const int* const table = p.c.table + b * p.c.pitch;
     bool poisoned = false;                                   // NaN codes were met where only some rows see them
@@ -189,26 +187,23 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
     // a tile with keys that some row does not see
     auto at_edge = [&](int key0, int at_v) __attribute__((always_inline)) {
         bool edge = at_v < 0;
-#pragma unroll
-        for (int r = 0; r < NR; ++r) edge = edge || key0 + kTile - 1 > hi[r] || (key0 < lo[r] && key0 + kTile > p.sinks);
+        edge = edge || key0 + kTile - 1 > hi || (key0 < lo && key0 + kTile > p.sinks);
         return __builtin_amdgcn_ballot_w64(edge) != 0;
     };
 
-    f32x4 sc[NR][4];
-    bf16x8 pf[NR][2];
+    f32x4 sc[4];
+    bf16x8 pf[2];
     auto scores = [&]() __attribute__((always_inline)) {
         const float scale = __uint_as_float(ke << 23);
 #pragma unroll
         for (int kt = 0; kt < 4; ++kt) {
-#pragma unroll
-            for (int r = 0; r < NR; ++r) sc[r][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            sc[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ch = 0; ch < KC; ++ch)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const bf16x8 kf = decode(kr[kt][ch][2 * u], kr[kt][ch][2 * u + 1], scale);
-#pragma unroll
-                    for (int r = 0; r < NR; ++r) sc[r][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[r][2 * ch + u], sc[r][kt], 0, 0, 0);
+                    sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[2 * ch + u], sc[kt], 0, 0, 0);
                 }
         }
     };
@@ -216,37 +211,33 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
         const int key0 = tile_of(t) * kTile;
         if (at_edge(key0, at_v)) {
             const int key = key0 + 16 * grp;                 // this lane's scores are those of 16 keys from here on
+            const unsigned visible = sees(key, hi, lo, at_v >= 0);
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                const unsigned visible = sees(key, hi[r], lo[r], at_v >= 0);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) sc[r][j / 4][j % 4] = visible >> j & 1 ? sc[r][j / 4][j % 4] : -INFINITY;
-            }
+            for (int j = 0; j < 16; ++j) sc[j / 4][j % 4] = visible >> j & 1 ? sc[j / 4][j % 4] : -INFINITY;
         }
+        float mx = sc[0][0];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) {
-            float mx = sc[r][0][0];
+        for (int j = 1; j < 16; ++j) mx = fmaxf(mx, sc[j / 4][j % 4]);
+        if (__builtin_amdgcn_ballot_w64(!(mx <= m_run + slack)) != 0) {
+            const float m_new = fmaxf(m_run, max_over_groups(mx));
+            const float alpha = exp2_hw((m_run - finite(m_new)) * c);
+            m_run = m_new;
+            l_run *= alpha;
 #pragma unroll
-            for (int j = 1; j < 16; ++j) mx = fmaxf(mx, sc[r][j / 4][j % 4]);
-            const float m_new = fmaxf(m_run[r], max_over_groups(mx));
-            const float m_use = m_new == -INFINITY ? 0.f : m_new;
-            const float alpha = exp2_hw((m_run[r] - m_use) * c), mc = m_use * c;
-            m_run[r] = m_new;
-            float sum = 0.f;
-            unsigned pk[8];
-#pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-                const float p0 = exp2_hw(fmaf(sc[r][j / 4][j % 4], c, -mc)), p1 = exp2_hw(fmaf(sc[r][j / 4][j % 4 + 1], c, -mc));
-                sum += p0 + p1;
-                pk[j / 2] = pack_bf16x2(p0, p1);
-            }
-            l_run[r] = l_run[r] * alpha + sum;
-            if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) oacc[r][d] *= alpha;
-            pf[r][0] = __builtin_bit_cast(bf16x8, (u32x4{pk[0], pk[1], pk[2], pk[3]}));
-            pf[r][1] = __builtin_bit_cast(bf16x8, (u32x4{pk[4], pk[5], pk[6], pk[7]}));
+            for (int d = 0; d < DT; ++d) oacc[d] *= alpha;
         }
+        const float mc = finite(m_run) * c;
+        float sum = 0.f;
+        unsigned pk[8];
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) {
+            const float p0 = exp2_hw(fmaf(sc[j / 4][j % 4], c, -mc)), p1 = exp2_hw(fmaf(sc[j / 4][j % 4 + 1], c, -mc));
+            sum += p0 + p1;
+            pk[j / 2] = pack_bf16x2(p0, p1);
+        }
+        l_run += sum;
+        pf[0] = __builtin_bit_cast(bf16x8, (u32x4{pk[0], pk[1], pk[2], pk[3]}));
+        pf[1] = __builtin_bit_cast(bf16x8, (u32x4{pk[4], pk[5], pk[6], pk[7]}));
     };
     auto weigh = [&](int t) __attribute__((always_inline)) {
         const int key0 = tile_of(t) * kTile;
@@ -270,8 +261,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const bf16x8 vf = decode(vr[d][2 * u], vr[d][2 * u + 1], scale);
-#pragma unroll
-                for (int r = 0; r < NR; ++r) oacc[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[r][u], oacc[r][d], 0, 0, 0);
+                oacc[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[u], oacc[d], 0, 0, 0);
             }
     };
 
@@ -302,51 +292,41 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
             const int key0 = tile_of(t) * kTile, key = key0 + 16 * grp;
             load_v(t, lookup(key));
             if (!at_edge(key0, at_v)) continue;
+            const unsigned visible = sees(key, hi, lo, at_v >= 0);
+            u32x4 see[2];
 #pragma unroll
-            for (int r = 0; r < NR; ++r) {
-                const unsigned visible = sees(key, hi[r], lo[r], at_v >= 0);
-                u32x4 see[2];
+            for (int j = 0; j < 8; ++j)
+                see[j / 4][j % 4] = (visible >> (2 * j) & 1) * 0x3f80u | (visible >> (2 * j + 1) & 1) * 0x3f800000u;     // ones in bf16
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    see[j / 4][j % 4] = (visible >> (2 * j) & 1) * 0x3f80u | (visible >> (2 * j + 1) & 1) * 0x3f800000u;     // ones in bf16
+            for (int d = 0; d < DT; ++d) {
+                f32x4 hits = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    f32x4 hits = {0.f, 0.f, 0.f, 0.f};
+                for (int u = 0; u < 2; ++u) {
+                    u32x4 ind;
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        u32x4 ind;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const unsigned nan = nan_codes(vr[d][2 * u + j / 2]) >> (16 * (j % 2) + 7);
-                            ind[j] = (nan & 1) * 0x3f80u | (nan >> 8 & 1) * 0x3f800000u;
-                        }
-                        hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ind), __builtin_bit_cast(bf16x8, see[u]), hits, 0, 0, 0);
+                    for (int j = 0; j < 4; ++j) {
+                        const unsigned nan = nan_codes(vr[d][2 * u + j / 2]) >> (16 * (j % 2) + 7);
+                        ind[j] = (nan & 1) * 0x3f80u | (nan >> 8 & 1) * 0x3f800000u;
                     }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) oacc[r][d][e] = hits[e] > 0.f ? NAN : oacc[r][d][e];
+                    hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ind), __builtin_bit_cast(bf16x8, see[u]), hits, 0, 0, 0);
                 }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) oacc[d][e] = hits[e] > 0.f ? NAN : oacc[d][e];
             }
         }
     }
 
     // merge the wavefronts: each scales its O to the maximum over all of them
-#pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        const float l = sum_over_groups(l_run[r]);
-        if (grp == 0) { s_ml[0][wave][r * kBlock + col] = m_run[r]; s_ml[1][wave][r * kBlock + col] = l; }
-    }
+    const float l = sum_over_groups(l_run);
+    if (grp == 0) { s_ml[0][wave][col] = m_run; s_ml[1][wave][col] = l; }
     __syncthreads();
+    float m = s_ml[0][0][col];
 #pragma unroll
-    for (int r = 0; r < NR; ++r) {
-        const int row = r * kBlock + col;
-        float m = s_ml[0][0][row];
+    for (int w = 1; w < NW; ++w) m = fmaxf(m, s_ml[0][w][col]);
+    const float f = m_run == -INFINITY ? 0.f : exp2_hw((m_run - m) * c);
+    if (first + col < R)
 #pragma unroll
-        for (int w = 1; w < NW; ++w) m = fmaxf(m, s_ml[0][w][row]);
-        const float f = m_run[r] == -INFINITY ? 0.f : exp2_hw((m_run[r] - m) * c);
-        if (first + row < R)
-#pragma unroll
-            for (int d = 0; d < DT; ++d) *(f32x4*)(s_o + (wave * ROWS + row) * PITCH + 16 * d + 4 * grp) = oacc[r][d] * f;
-    }
+        for (int d = 0; d < DT; ++d) *(f32x4*)(s_o + (wave * ROWS + col) * PITCH + 16 * d + 4 * grp) = oacc[d] * f;
     if (tid < ROWS && first + tid < R) {
         const int row = first + tid, i = row / g, h = row - i * g;
         const size_t rowi = ((size_t)b * p.Hq + hk * g + h) * p.Sq + i;
@@ -400,12 +380,13 @@ template <int PIECES> __device__ __forceinline__ constexpr int piece_offset(int 
     return row * PIECES * 16 + ((piece ^ (PIECES == 16 ? row & 15 : (row >> 1) & 7)) << 4);
 }
 
-template <int D, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
+constexpr int kTileWaves = 4;
+template <int D>
+__global__ __launch_bounds__(kTileWaves * 64, 2) void attn_kv_tiles(KvAttnParams p) {
     constexpr int KS = D / 16, DB = D / 32, KP = D / 8;
-    constexpr int NC = D * kTile / 16 / (NW * 64);        // 16-code pieces per thread, tile and matrix
+    constexpr int NC = D / 64;                            // 16-code pieces per thread, tile and matrix
     constexpr int STAGE = 2 * kTile * D * 2;              // bytes of a K and a V tile
-    constexpr int ROWS = NW * kTileRows;
+    constexpr int ROWS = kTileWaves * kTileRows;
     __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
     // by stage, the last tile: whose group of 16 keys has no page; whose V has a NaN, and which (for tiles at an edge only)
     __shared__ __attribute__((aligned(16))) int s_gone[2][4];
@@ -448,47 +429,51 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
         return t < whole ? a0 + t : z;
     };
 
-    // A wavefront's pieces lie in one page each: K piece n is key k_key + 8 (D 64: 16) n, codes from 16 k_c on; V piece n the 16
-    // keys of group v_grp, row v_row + 64 n.  So page numbers and addresses are scalars.
+    // Wavefront w decodes the 16 keys of group w, which lie in one page: the page's number, addresses and exponents are scalars.  K
+    // piece n is key 16 w + k_row + 8 n (D = 128), codes from 16 k_c on; V piece n the 16 keys of row v_row + 64 n.
+    // (Which lane has which piece: eight lanes side by side write to eight different places of 16 bytes modulo 128.)
     constexpr int KPI = 1024 / D;                         // keys per load of a wavefront
     const int page = p.c.page, page_log2 = p.c.page_log2;
-    const int k_first = wave * (kTile / NW), k_key = k_first + lane / (D / 16), k_c = lane % (D / 16);
-    const int v_grp = wave & 3, v_row = (wave >> 2) * NC * 64 + lane;
-    typedef const int __attribute__((address_space(4))) * ScalarInts;
-    const ScalarInts table = (ScalarInts)(p.c.table + b * p.c.pitch);
-    int at_k, at_v;                                       // the pages of the tile that is loaded next, -1: none
+    const int k_c = D == 128 ? (lane & 3) | (lane >> 1 & 4) : lane & 3;
+    const int k_row = D == 128 ? (lane >> 2 & 1) | (lane >> 3 & 6) : (lane >> 1 & 2) | (lane >> 3 & 1) | (lane >> 2 & 12);
+    const int v_row = lane << 1 & 14 | (lane >> 3 & 1) | (lane & 48);
+    typedef const unsigned __attribute__((address_space(4))) * ScalarWords;
+    const ScalarWords table = (ScalarWords)(p.c.table + b * p.c.pitch);
+    const unsigned page_bytes = page * D;
+    const int last_slot = (seen.n - 1) >> page_log2;
+    int key;                                              // the first key of the group, in the tile that is loaded next,
+    unsigned entry;                                       // and its table entry
     u32x4 kr[NC], vr[NC];
-    unsigned ke, ve;                                      // biased exponents
-    bool gap;                                             // whether the loaded V piece has no page
-    auto lookup = [&](int key) __attribute__((always_inline)) {
-        const int at = table[min(key, seen.n - 1) >> page_log2];
-        return key < seen.n && (unsigned)at < (unsigned)p.c.P ? at : -1;
-    };
+    unsigned ke, ve, shifts;                              // words with the loaded tile's biased exponents, and where in them
+    bool gap;                                             // whether the loaded group has no page
     auto find = [&](int t) __attribute__((always_inline)) {           // (behind the last tile: the last one again)
-        const int key0 = tile_of(min(t, t1 - 1)) * kTile;
-        at_k = lookup(key0 + k_first);
-        at_v = lookup(key0 + 16 * v_grp);
+        key = tile_of(min(t, t1 - 1)) * kTile + 16 * wave;
+        entry = table[min(key >> page_log2, last_slot)];
     };
-    const unsigned k_lane = lane / (D / 16) * D + 16 * k_c, v_lane = v_row * page;
-    auto load = [&](int t) __attribute__((always_inline)) {
-        const int key0 = tile_of(min(t, t1 - 1)) * kTile;
-        const size_t unit_k = (size_t)max(at_k, 0) * p.c.Hkv + hk, unit_v = (size_t)max(at_v, 0) * p.c.Hkv + hk;
-        const unsigned char* const k = p.c.k + (unit_k * page + ((key0 + k_first) & (page - 1))) * D;
-        const unsigned char* const v = p.c.v + unit_v * page * D + ((key0 + 16 * v_grp) & (page - 1));
+    const unsigned k_lane = k_row * D + 16 * k_c, v_lane = v_row * page;
+    // (The exponents come by scalar loads: those are counted apart from the codes' loads, so that none of these is waited for early.
+    // A byte's aligned word lies in the byte's own allocation, whatever its neighbours are.)
+    auto load = [&]() __attribute__((always_inline)) {
+        gap = !((int)(key < seen.n) & (int)(entry < (unsigned)p.c.P));
+        const unsigned unit = (gap ? 0u : entry) * p.c.Hkv + hk;
+        const unsigned long long at = (unsigned long long)unit * page_bytes;
+        const unsigned char* const k = p.c.k + at + (key & (page - 1)) * D;
+        const unsigned char* const v = p.c.v + at + (key & (page - 1));
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
             kr[n] = *(const u32x4*)(k + k_lane + n * KPI * D);
             vr[n] = *(const u32x4*)(v + v_lane + n * 64 * page);
         }
-        ke = p.c.ke[unit_k];
-        ve = p.c.ve[unit_v];
-        gap = at_v < 0;
+        const unsigned long long ea = (unsigned long long)(p.c.ke + unit), va = (unsigned long long)(p.c.ve + unit);
+        ke = *(ScalarWords)(ea & ~3ull);
+        ve = *(ScalarWords)(va & ~3ull);
+        shifts = (unsigned)(ea & 3) | (unsigned)(va & 3) << 8;
     };
     // What tile t, loaded, needs before it is decoded: zeros where the sequence holds nothing, a note of groups without a page.
     // At an edge NaN must not meet the probability 0 of a row that does not see it: zeros too, and a note.
     auto mend = [&](int t) __attribute__((always_inline)) {
         if (t < whole && !gap) return;
-        const int key0 = tile_of(min(t, t1 - 1)) * kTile, left = gap ? 0 : seen.n - (key0 + 16 * v_grp);
+        const int left = gap ? 0 : seen.n - (tile_of(min(t, t1 - 1)) * kTile + 16 * wave);
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
             unsigned bits = 0;
@@ -502,18 +487,18 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
                 vr[n][j] = w;
             }
             if (t >= whole) {
-                s_bits[t & 1][v_row + 64 * n][v_grp] = (unsigned short)bits;
+                s_bits[t & 1][v_row + 64 * n][wave] = (unsigned short)bits;
                 if (bits) s_nan[t & 1] = t;
             }
         }
-        if (gap) s_gone[t & 1][v_grp] = t;
+        if (gap) s_gone[t & 1][wave] = t;
     };
     // Lane offsets into a stage; the pieces of a row are found by exchanging address bits.
     unsigned k_read = piece_offset<KP>(key_of_row(lane & 31), half), v_read = kTile * D * 2 + piece_offset<8>(lane & 31, half);
-    unsigned k_write = piece_offset<KP>(k_key, 2 * k_c), v_write = kTile * D * 2 + piece_offset<8>(v_row, 2 * v_grp);
+    unsigned k_write = piece_offset<KP>(16 * wave + k_row, 2 * k_c), v_write = kTile * D * 2 + piece_offset<8>(v_row, 2 * wave);
     auto put = [&](int t) __attribute__((always_inline)) {
         const unsigned st = (t & 1) * STAGE;
-        const float ks = __uint_as_float(ke << 23), vs = __uint_as_float(ve << 23);
+        const float ks = __uint_as_float((ke >> (8 * (shifts & 3)) & 0xff) << 23), vs = __uint_as_float((ve >> (8 * (shifts >> 8)) & 0xff) << 23);
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
             // (K rows n KPI further on: for D = 128 their pieces' places differ in bit 3)
@@ -543,10 +528,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) oacc[i][e] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
-    const float c = p.scale_log2;
+    const float c = p.scale_log2, slack = kSlack / c;
 
     f32x16 sc[2];
-    bf16x8 pf[4];
     auto scores = [&](int t) __attribute__((always_inline)) {
         const unsigned at = k_read + (t & 1) * STAGE;
 #pragma unroll
@@ -560,40 +544,56 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
             }
         }
     };
-    auto softmax = [&]() __attribute__((always_inline)) {
+    // what is under way moves on by a tile
+    auto advance = [&](int t) __attribute__((always_inline)) { put(t + 1); load(); find(t + 3); };
+    // The probabilities of the two blocks of 32 keys, and O += V^T P^T: the second block's probabilities are made between the
+    // first one's matrix instructions.
+    auto weigh = [&](int t) __attribute__((always_inline)) {
         float mx = sc[0][0];
 #pragma unroll
         for (int j = 1; j < 32; ++j) mx = fmaxf(mx, sc[j / 16][j % 16]);
-        const float m_new = fmaxf(m_run, max_across_halves(mx));
-        const float m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = exp2_hw((m_run - m_use) * c), mc = m_use * c;
-        m_run = m_new;
-        float sum = 0.f;
-        unsigned pk[16];
-#pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-            const float p0 = exp2_hw(fmaf(sc[j / 16][j % 16], c, -mc)), p1 = exp2_hw(fmaf(sc[j / 16][j % 16 + 1], c, -mc));
-            sum += p0 + p1;
-            pk[j / 2] = pack_bf16x2(p0, p1);
-        }
-        l_run = l_run * alpha + sum;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) pf[kk] = __builtin_bit_cast(bf16x8, (u32x4{pk[4 * kk], pk[4 * kk + 1], pk[4 * kk + 2], pk[4 * kk + 3]}));
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0)
+        if (__builtin_amdgcn_ballot_w64(!(mx <= m_run + slack)) != 0) {
+            const float m_new = fmaxf(m_run, max_across_halves(mx));
+            const float alpha = exp2_hw((m_run - finite(m_new)) * c);
+            m_run = m_new;
+            l_run *= alpha;
 #pragma unroll
             for (int i = 0; i < DB; ++i)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) oacc[i][e] *= alpha;
-    };
-    auto weigh = [&](int t) __attribute__((always_inline)) {
+        }
+        const float mc = finite(m_run) * c;
         const unsigned at = v_read + (t & 1) * STAGE;
+        auto v_piece = [&](int kk, int i) __attribute__((always_inline)) { return *(const bf16x8*)(smem + (at ^ (kk << 5)) + 32 * i * 128); };
+        unsigned pk[16];
+        auto two = [&](int j) __attribute__((always_inline)) {                // probabilities 2 j and 2 j + 1
+            const float p0 = exp2_hw(fmaf(sc[j / 8][2 * j % 16], c, -mc)), p1 = exp2_hw(fmaf(sc[j / 8][2 * j % 16 + 1], c, -mc));
+            l_run += p0 + p1;
+            pk[j] = pack_bf16x2(p0, p1);
+        };
+        auto p_piece = [&](int kk) __attribute__((always_inline)) { return __builtin_bit_cast(bf16x8, (u32x4{pk[4 * kk], pk[4 * kk + 1], pk[4 * kk + 2], pk[4 * kk + 3]})); };
+        bf16x8 vf[2][DB];
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk)
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int i = 0; i < DB; ++i) vf[kk][i] = v_piece(kk, i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) two(j);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
             for (int i = 0; i < DB; ++i) {
-                const bf16x8 vf = *(const bf16x8*)(smem + (at ^ (kk << 5)) + 32 * i * 128);
-                oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[kk], oacc[i], 0, 0, 0);
+                oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[kk][i], p_piece(kk), oacc[i], 0, 0, 0);
+                vf[kk][i] = v_piece(kk + 2, i);
+#pragma unroll
+                for (int j = 0; j < 4 / DB; ++j) two(8 + (kk * DB + i) * (4 / DB) + j);
+                __builtin_amdgcn_sched_barrier(0);
             }
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+            for (int i = 0; i < DB; ++i) oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[kk][i], p_piece(kk + 2), oacc[i], 0, 0, 0);
     };
     // a NaN for every row that sees one
     auto poison = [&](int t, unsigned visible) __attribute__((always_inline)) {
@@ -624,17 +624,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
 
     if (t0 < t1) {
         if (tid < 8) { s_nan[tid & 1] = -1; s_gone[tid & 1][tid >> 1] = -1; }
-        find(t0); load(t0); find(t0 + 1);
+        find(t0); load(); find(t0 + 1);
         barrier();
-        mend(t0); put(t0); load(t0 + 1); find(t0 + 2);
+        mend(t0); put(t0); load(); find(t0 + 2);
         barrier();
     }
     auto groups = [&](int t) __attribute__((always_inline)) {                // which groups of 16 keys have a page
-        const i32x4 gone = *(const i32x4*)s_gone[t & 1];
-        unsigned there = 15;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) if (__builtin_amdgcn_readfirstlane(gone[x]) == t) there &= ~(1u << x);
-        return there;
+        return ~(unsigned)__builtin_amdgcn_ballot_w64(lane < 4 && s_gone[t & 1][lane & 3] == t) & 15;
     };
     int t = t0;
     for (; t < min(t1, whole); ++t) {
@@ -642,8 +638,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
         if (groups(t) != 15) break;                                          // a page is missing: the general loop goes on
         mend(t + 1);
         scores(t);
-        put(t + 1); load(t + 2); find(t + 3);
-        softmax();
+        advance(t);
         weigh(t);
         barrier();
     }
@@ -652,14 +647,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_tiles(KvAttnParams p) {
         const int key0 = tile_of(t) * kTile;
         const unsigned there = groups(t);
         mend(t + 1);
-        put(t + 1); load(t + 2); find(t + 3);
+        advance(t);
         // nothing for this wavefront behind its last row's position, or in front of its first row's window
         if (key0 <= w_hi && (key0 + kTile > w_lo || key0 < p.sinks)) {
             scores(t);
             const unsigned visible = seen_keys(key0, there);
 #pragma unroll
             for (int j = 0; j < 32; ++j) sc[j / 16][j % 16] = visible >> j & 1 ? sc[j / 16][j % 16] : -INFINITY;
-            softmax();
             weigh(t);
             if (__builtin_amdgcn_readfirstlane(s_nan[t & 1]) == t) poison(t, visible);
         }
@@ -759,31 +753,62 @@ __global__ __launch_bounds__(256) void attn_kv_combine(KvAttnParams p) {
 
 }  // namespace
 
-// Rows per workgroup: 16 where that is all there is, else 32 rows per wavefront that share decoded tiles.
+// Time of a call in microseconds, from what was measured on shapes of 1 to 128 sequences, 300 to 64000 keys, 1 to 256 packed rows.
+// A round of workgroups takes its start (lengths, page numbers, first codes) and end, and for its tiles the longer of what their
+// arithmetic takes, which two workgroups of four wavefronts on a CU share, and of what HBM takes at 6.2 TB/s, or up to 1.4
+// times that where both are alike.  Parts cost a second kernel and their traffic.
+static double estimate(const KvAttnPlan& plan, long long pairs, long long rows, int tiles, int D) {
+    const bool rows16 = plan.rows == kBlock, wide = D == 128;
+    const long long n = pairs * plan.row_wgs * plan.splits, slots = rows16 && plan.waves == 8 ? 256 : rows16 && !wide ? 768 : 512;
+    const double start = rows16 ? (plan.waves == 8 ? (wide ? 6.6 : 5.6) : wide ? 5.2 : 4.8) : 6.5;
+    // a step is a tile of every wavefront (rows) or of the workgroup: with one workgroup on a CU, and with the CU full
+    const double alone = rows16 ? (plan.waves == 8 ? (wide ? 2.5 : 1.0) : wide ? 1.3 : 0.72) : wide ? 1.21 : 0.95;
+    const double full = rows16 ? (plan.waves == 8 ? alone : wide ? 2.1 : 1.6) : wide ? 2.07 : 1.36;
+    const int per = (tiles + plan.splits - 1) / plan.splits, steps = rows16 ? (per + plan.waves - 1) / plan.waves : per;
+    const double bytes = (double)tiles / plan.splits * kTile * D * 2 / plan.row_wgs;          // of a workgroup, its row blocks sharing an L2
+    auto round = [&](long long wgs) {
+        const double work = steps * (wgs <= 256 ? alone : full), hbm = wgs * bytes / 6.2e6;
+        const double both = sqrt(work * work + hbm * hbm) * (rows16 && plan.waves == 8 ? 0.9 : 1.0);
+        return start + (both > work ? (both > hbm ? both : hbm) : work);
+    };
+    double t = (double)(n / slots) * (n >= slots ? round(slots) : 0.0);
+    if (n % slots) t += round(n % slots);
+    if (plan.splits > 1) t += 4.2 + rows * 0.0008 + (double)rows * plan.splits * (D + 2) * 1.6e-6;
+    return t;
+}
+
+// How many rows a workgroup takes, by how many wavefronts, and how the keys are cut: whatever is estimated to be the fastest.
+// Measured, rows of 16 / of 128 per workgroup, sequences x keys, D = 128, 8 kv heads: 32 packed rows 1 x 64000 35.5 / 47.0 us,
+// 64 x 1000 39.5 / 45.0; 64 rows 55.9 / 50.2, 61.1 / 46.6; 128 rows 96.6 / 57.4, but 1 x 1000 11.6 / 16.2.
 KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits) {
-    KvAttnPlan plan;
-    const long long R = (long long)(Hq / Hkv) * Sq;
-    plan.rows = R <= kBlock ? kBlock : 4 * kTileRows;
-    plan.waves = plan.rows == kBlock && (long long)B * Hkv < 512 ? 8 : 4;
-    plan.row_wgs = (int)((R + plan.rows - 1) / plan.rows);
-    plan.splits = splits;
-    plan.keys = keys;
-    if (splits == 0) {
-        const int tiles = (keys + kTile - 1) / kTile, most = plan.rows == kBlock ? (tiles + plan.waves - 1) / plan.waves : (tiles + 3) / 4;
-        const long long base = (long long)B * Hkv * plan.row_wgs;
-        long long s = (plan.rows == kBlock ? 512 : 512) / base;
-        if (s > most) s = most;
-        plan.splits = s < 1 ? 1 : s > kMaxKvSplits ? kMaxKvSplits : (int)s;
+    static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
+    const long long R = (long long)(Hq / Hkv) * Sq, pairs = (long long)B * Hkv, rows = (long long)B * Hq * Sq;
+    const int tiles = (keys + kTile - 1) / kTile;
+    KvAttnPlan best{};
+    double least = 1e300;
+    for (int kind = R <= 512 ? 0 : 2; kind < 3; ++kind) {
+        KvAttnPlan plan;
+        plan.rows = kind < 2 ? kBlock : kTileWaves * kTileRows;
+        plan.waves = kind == 0 ? 8 : 4;
+        plan.row_wgs = (int)((R + plan.rows - 1) / plan.rows);
+        plan.keys = keys;
+        const int most = kind < 2 ? (tiles + plan.waves - 1) / plan.waves : (tiles + 1) / 2;
+        for (int cut : kCuts) {
+            if (splits == 0 && cut > 1 && cut > most) break;
+            plan.splits = splits ? splits : cut;
+            const double t = estimate(plan, pairs, rows, tiles, D);
+            if (t < least) { least = t; best = plan; }
+            if (splits) break;
+        }
     }
-    (void)D;
-    return plan;
+    return best;
 }
 
 template <int D>
 static void launch(const KvAttnParams& p, const KvAttnPlan& plan, unsigned blocks, hipStream_t stream) {
-    if (plan.rows == kBlock && plan.waves == 8) hipLaunchKernelGGL((attn_kv_rows<D, 1, 8>), dim3(blocks), dim3(512), 0, stream, p);
-    else if (plan.rows == kBlock) hipLaunchKernelGGL((attn_kv_rows<D, 1, 4>), dim3(blocks), dim3(256), 0, stream, p);
-    else hipLaunchKernelGGL((attn_kv_tiles<D, 4>), dim3(blocks), dim3(256), 0, stream, p);
+    if (plan.rows == kBlock && plan.waves == 8) hipLaunchKernelGGL((attn_kv_rows<D, 8>), dim3(blocks), dim3(512), 0, stream, p);
+    else if (plan.rows == kBlock) hipLaunchKernelGGL((attn_kv_rows<D, 4>), dim3(blocks), dim3(256), 0, stream, p);
+    else hipLaunchKernelGGL(attn_kv_tiles<D>, dim3(blocks), dim3(kTileWaves * 64), 0, stream, p);
 }
 
 int attn_kv_launch(KvAttnParams p, const KvAttnPlan& plan, hipStream_t stream) {
