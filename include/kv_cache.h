@@ -51,7 +51,7 @@ typedef struct KvFp8Cache {
  * the NaN code 0x7f.  Where e' > e the codes of the page's earlier tokens are rounded again to c * 2^(e - e').  All other
  * positions, those behind the last new token among them, keep their codes.
  * count outside 0 ... S is taken as the nearer end, positions outside the table are dropped.  A page that a call writes
- * belongs to one sequence of it: two sequences that write the same page leave it in no defined state.
+ * stands once in the table: written as two pages, of one sequence or of two, it is left in no defined state.
  * Errors: NULL_PTR, BAD_SHAPE, UNSUPPORTED (D, page), MISALIGNED, LAUNCH.
  */
 int kv_fp8_write(const KvFp8Cache *cache, const void *k, const void *v,
@@ -90,8 +90,10 @@ int kv_fp8_read(const KvFp8Cache *cache, const int *table, long long table_pitch
  * library's choice, at most 256; splits > 1 needs 4 * B * Hq * Sq * splits * (D + 2) bytes.  With a NULL or too small
  * workspace, or splits = 1, the keys are not cut: the same result up to the order of fp32 sums.  Parts are added in a
  * fixed order: results do not vary from run to run.
- * Supported: Hq a multiple of Hkv, Hq / Hkv * Sq < 2^28, B * Hq * Sq < 2^31; scale finite and > 0; window, sinks >= 0.
- * Errors: NULL_PTR, BAD_SHAPE, UNSUPPORTED (D, page, splits), MISALIGNED (q, o, workspace 16 bytes; lse, lens, table 4),
+ * wg_rows, for tuning and for tests that run every shape both ways: query rows (heads of one kv head side by side) per
+ * workgroup, 16, 128, or 0 = the library's choice.
+ * Supported: Hq a multiple of Hkv, Hq / Hkv * Sq < 2^28, B * Hq * Sq < 2^31 (cut: 2^24); scale finite and > 0; window, sinks >= 0.
+ * Errors: NULL_PTR, BAD_SHAPE, UNSUPPORTED (D, page, splits, wg_rows), MISALIGNED (q, o, workspace 16 bytes; lse, lens, table 4),
  * BAD_SCALE, LAUNCH.
  */
 size_t attn_kv_fp8_workspace_bytes(int B, int Hq, int Hkv, int Sq, int max_len, int D, int window, int sinks);
@@ -100,7 +102,7 @@ int attn_kv_fp8(const void *q, const KvFp8Cache *cache, const int *table, long l
                 const int *lens, const int *q_lens, void *o, float *lse, int B, int Hq, int Sq,
                 const long long *q_strides, const long long *o_strides,
                 int causal, int window, int sinks, float scale, int max_len,
-                void *workspace, size_t workspace_bytes, int splits, void *stream);
+                void *workspace, size_t workspace_bytes, int splits, int wg_rows, void *stream);
 
 #ifdef __cplusplus
 }

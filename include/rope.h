@@ -12,8 +12,8 @@
  *
  * Columns R ... D-1 are copied.  inverse != 0 turns by the opposite angle (s changes its sign): the transposed rotation,
  * which is the gradient of the operation with respect to x (times mscale, as the operation itself).
- * The angle is formed and reduced to a part of a turn in 64 bits, so that it is as exact at position 2^31 - 1 as at 0;
- * sine, cosine and the products are fp32, every result is rounded once to bf16 (nearest even).
+ * The angle is formed and reduced to a part of a turn in 64 bits, so that at frequencies of up to one radian per position it
+ * is off by less than 2^-20 at any position; sine, cosine and the products are fp32, every result is rounded once to bf16 (nearest even).
  *
  * DEVICE pointers, caller-owned:
  *     q, q_out   bf16 [B, Hq, S, D]      k, k_out  bf16 [B, Hk, S, D], both NULL (and Hk 0): only q

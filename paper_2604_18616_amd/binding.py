@@ -78,7 +78,7 @@ def load_library(build_if_missing: bool = True):
         lib.attn_kv_fp8_workspace_bytes.restype = ctypes.c_size_t
         lib.attn_kv_fp8_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i]
         lib.attn_kv_fp8.restype = i
-        lib.attn_kv_fp8.argtypes = [p, p, p, ll, i, p, p, p, p, i, i, i, p, p, i, i, i, f, i, p, ctypes.c_size_t, i, p]
+        lib.attn_kv_fp8.argtypes = [p, p, p, ll, i, p, p, p, p, i, i, i, p, p, i, i, i, f, i, p, ctypes.c_size_t, i, i, p]
         lib.rope_bf16.restype = i
         lib.rope_bf16.argtypes = [p, p, p, p, i, i, i, i, i, i, p, p, p, p, p, ll, p, i, i, f, p]
         lib.rope_frequencies.restype = i
@@ -260,7 +260,7 @@ def attn_fwd(q, k, v, o=None, lse=None, causal=False, scale=None, stream=None):
     if ws is not None:
         rc = lib.attn_fwd_workspace(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
                                     B, Hq, Hkv, Sq, Sk, D, _Int64x3(*qst[:3]), _Int64x3(*kst[:3]), _Int64x3(*vst[:3]), _Int64x3(*ost[:3]),
-                                    causal, scale, ws.data_ptr(), need, need // (4 * B * Hq * Sq * (D + 2)), stream)
+                                    causal, scale, ws.data_ptr(), need, 0 if wg_rows else need // (4 * B * Hq * Sq * (D + 2)), int(wg_rows), stream)
     elif q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and o.is_contiguous():
         rc = lib.attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
                           B, Hq, Hkv, Sq, Sk, D, causal, scale, stream)
@@ -512,13 +512,14 @@ def kv_fp8_read(cache, table, lens, S, first=0, k=None, v=None, stream=None):
     return k, v
 
 
-def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=False, window=0, sinks=0, scale=None, max_len=0, stream=None):
+def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=False, window=0, sinks=0, scale=None, max_len=0, stream=None, wg_rows=0):
     """O, LSE = attention of bf16 q [B, Hq, Sq, D] over a quantised cache: sequence b's lens[b] keys and values, of which the
     q_lens[b] (all Sq where None) query rows are the last.  causal: row i sees the keys up to its own position; window > 0: of
     those only the last `window` and the sequence's `sinks` first.  Rows that see nothing and rows from q_lens[b] on get O = 0
     and LSE = -inf.  lens, q_lens int32 [B] on the GPU; max_len: no sequence is longer (0: the table's width).
-    o and lse as in attn_fwd.  Enqueued on `stream` (default: torch's current stream); no sync."""
-    if o is None and lse is None and stream is None:
+    o and lse as in attn_fwd.  wg_rows: 0 (by size), 16 or 128 query rows per workgroup.  Enqueued on `stream` (default: torch's
+    current stream); no sync."""
+    if o is None and lse is None and stream is None and wg_rows == 0:
         native = _plain_calls(q)
         done = native.attn_kv(q, cache, table, lens, q_lens, causal, window, sinks, scale, max_len) if native else None
         if done is not None:
@@ -549,7 +550,7 @@ def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=Fal
     with _on(device):
         rc = lib.attn_kv_fp8(q.data_ptr(), ctypes.byref(struct), at, pitch, width, lens, q_lens, o.data_ptr(), lse.data_ptr(), B, Hq, Sq, qs, os_,
                              1 if causal else 0, window, sinks, scale, max_len, None if ws is None else ws.data_ptr(), 0 if ws is None else need,
-                             1 if ws is None else need // (4 * B * Hq * Sq * (D + 2)), stream)
+                             1 if ws is None else 0 if wg_rows else need // (4 * B * Hq * Sq * (D + 2)), int(wg_rows), stream)
     if rc != 0:
         raise AttnError(rc, strerror(rc))
     return o, lse

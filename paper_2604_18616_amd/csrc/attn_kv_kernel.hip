@@ -780,15 +780,16 @@ static double estimate(const KvAttnPlan& plan, long long pairs, long long rows, 
 // How many rows a workgroup takes, by how many wavefronts, and how the keys are cut: whatever is estimated to be the fastest.
 // Measured, rows of 16 / of 128 per workgroup, sequences x keys, D = 128, 8 kv heads: 32 packed rows 1 x 64000 35.5 / 47.0 us,
 // 64 x 1000 39.5 / 45.0; 64 rows 55.9 / 50.2, 61.1 / 46.6; 128 rows 96.6 / 57.4, but 1 x 1000 11.6 / 16.2.
-KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits) {
+KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits, int wg_rows) {
     static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
     const long long R = (long long)(Hq / Hkv) * Sq, pairs = (long long)B * Hkv, rows = (long long)B * Hq * Sq;
     const int tiles = (keys + kTile - 1) / kTile;
     KvAttnPlan best{};
     double least = 1e300;
-    for (int kind = R <= 512 ? 0 : 2; kind < 3; ++kind) {
+    for (int kind = 0; kind < 3; ++kind) {
         KvAttnPlan plan;
         plan.rows = kind < 2 ? kBlock : kTileWaves * kTileRows;
+        if (wg_rows ? plan.rows != wg_rows : kind < 2 && R > 512) continue;
         plan.waves = kind == 0 ? 8 : 4;
         plan.row_wgs = (int)((R + plan.rows - 1) / plan.rows);
         plan.keys = keys;
@@ -796,7 +797,8 @@ KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int spl
         for (int cut : kCuts) {
             if (splits == 0 && cut > 1 && cut > most) break;
             plan.splits = splits ? splits : cut;
-            const double t = estimate(plan, pairs, rows, tiles, D);
+            // (a given cut that is the library's own gets the shape that the library chose for it)
+            const double t = estimate(plan, pairs, rows, tiles, D) + (plan.splits > 1 && plan.splits > most ? 1e9 : 0.0);
             if (t < least) { least = t; best = plan; }
             if (splits) break;
         }
@@ -815,7 +817,7 @@ int attn_kv_launch(KvAttnParams p, const KvAttnPlan& plan, hipStream_t stream) {
     p.row_wgs = plan.row_wgs; p.splits = plan.splits;
     p.most_tiles = (plan.keys + kTile - 1) / kTile;
     const double blocks = (double)p.B * p.c.Hkv * p.row_wgs * p.splits;
-    if (blocks * 512 >= 4294967296.0) return -2;
+    if (blocks * 512 >= 4294967296.0 || (p.splits > 1 && (double)p.B * p.Hq * p.Sq * 256 >= 4294967296.0)) return -2;
     if (p.c.D == 128) launch<128>(p, plan, (unsigned)blocks, stream);
     else launch<64>(p, plan, (unsigned)blocks, stream);
     if (hipGetLastError() != hipSuccess) return -1;

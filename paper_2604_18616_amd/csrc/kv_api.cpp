@@ -88,20 +88,20 @@ static int check_rows(int B, int Hq, int Hkv, int Sq) {
 
 extern "C" size_t attn_kv_fp8_workspace_bytes(int B, int Hq, int Hkv, int Sq, int max_len, int D, int window, int sinks) {
     if (check_rows(B, Hq, Hkv, Sq) || check_sizes(Hkv, D, 16) || max_len <= 0 || max_len >= (1 << 30) || window < 0 || sinks < 0) return 0;
-    return part_bytes(B, Hq, Sq, D, attn_kv_plan(B, Hq, Hkv, Sq, keys_seen(Sq, max_len, window, sinks), D, 0).splits);
+    return part_bytes(B, Hq, Sq, D, attn_kv_plan(B, Hq, Hkv, Sq, keys_seen(Sq, max_len, window, sinks), D, 0, 0).splits);
 }
 
 extern "C" int attn_kv_fp8(const void* q, const KvFp8Cache* cache, const int* table, long long table_pitch, int width,
                            const int* lens, const int* q_lens, void* o, float* lse, int B, int Hq, int Sq,
                            const long long* qs, const long long* os,
                            int causal, int window, int sinks, float scale, int max_len,
-                           void* workspace, size_t workspace_bytes, int splits, void* stream) {
+                           void* workspace, size_t workspace_bytes, int splits, int wg_rows, void* stream) {
     if (!q || !o || !lens || !qs || !os) return ATTN_ERR_NULL_PTR;
     KvAttnParams p;
     if (int rc = pages_of(cache, table, table_pitch, width, &p.c)) return rc;
     if (int rc = check_rows(B, Hq, p.c.Hkv, Sq)) return rc;
     if (window < 0 || sinks < 0 || max_len < 0) return ATTN_ERR_BAD_SHAPE;
-    if (splits < 0 || splits > kMaxKvSplits) return ATTN_ERR_UNSUPPORTED;
+    if (splits < 0 || splits > kMaxKvSplits || (wg_rows != 0 && wg_rows != 16 && wg_rows != 128)) return ATTN_ERR_UNSUPPORTED;
     if (((uintptr_t)q | (uintptr_t)o | (uintptr_t)workspace) & 15u) return ATTN_ERR_MISALIGNED;
     if (((uintptr_t)lse | (uintptr_t)lens | (uintptr_t)q_lens) & 3u) return ATTN_ERR_MISALIGNED;
     if (int rc = check_strides(qs, p.c.D)) return rc;
@@ -119,9 +119,9 @@ extern "C" int attn_kv_fp8(const void* q, const KvFp8Cache* cache, const int* ta
     p.scale = scale;
     p.scale_log2 = (float)((double)scale * 1.4426950408889634074);
     const int keys = keys_seen(Sq, p.max_len, window, sinks);
-    KvAttnPlan plan = attn_kv_plan(B, Hq, p.c.Hkv, Sq, keys, p.c.D, splits);
+    KvAttnPlan plan = attn_kv_plan(B, Hq, p.c.Hkv, Sq, keys, p.c.D, splits, wg_rows);
     if (!workspace || workspace_bytes < part_bytes(B, Hq, Sq, p.c.D, plan.splits))
-        plan = attn_kv_plan(B, Hq, p.c.Hkv, Sq, keys, p.c.D, 1);
+        plan = attn_kv_plan(B, Hq, p.c.Hkv, Sq, keys, p.c.D, 1, wg_rows);
     p.part = (float*)workspace;
     p.ml = plan.splits > 1 ? p.part + (size_t)B * Hq * Sq * plan.splits * p.c.D : nullptr;
     return answer(attn_kv_launch(p, plan, (hipStream_t)stream));

@@ -48,8 +48,8 @@ struct KvAttnParams {
 int kv_write_launch(const KvWriteParams& p, hipStream_t stream);
 int kv_read_launch(const KvReadParams& p, hipStream_t stream);
 
-// How a call's rows and keys are cut; splits 0: by size.  Host arithmetic only.
+// How a call's rows and keys are cut; splits, wg_rows 0: by size.  Host arithmetic only.
 constexpr int kMaxKvSplits = 256;
 struct KvAttnPlan { int rows, waves, row_wgs, splits, keys; };       // rows: packed query rows per workgroup; keys: that they can see
-KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits);
+KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits, int wg_rows);
 int attn_kv_launch(KvAttnParams p, const KvAttnPlan& plan, hipStream_t stream);

@@ -218,7 +218,7 @@ PyObject* attn_kv(PyObject*, PyObject* const* args, Py_ssize_t n) {   // q, cach
             if (need) ws = scratch(need, q);
             rc = entry.attn_kv_fp8(q.data_ptr(), &c.c, c.table, c.pitch, (int)c.W, lens, q_lens, o.data_ptr(), (float*)lse.data_ptr(), (int)B, (int)Hq, (int)Sq,
                                    strides(q).s, strides(o).s, causal, window, sinks, (float)scale, max_len, ws.defined() ? ws.data_ptr() : nullptr,
-                                   ws.defined() ? need : 0, ws.defined() ? (int)(need / (4 * (size_t)B * Hq * Sq * (D + 2))) : 1, stream_of(q));
+                                   ws.defined() ? need : 0, ws.defined() ? (int)(need / (4 * (size_t)B * Hq * Sq * (D + 2))) : 1, 0, stream_of(q));
         }
     }
     if (rc == INT_MIN) Py_RETURN_NONE;

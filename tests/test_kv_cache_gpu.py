@@ -36,6 +36,9 @@ CASES = [
     (2, 2, 128, 300, 128, [0, 200], [299, 300]),
     (4, 1, 128, 40, 16, [3, 0, 16, 100], [0, 40, -5, 1000]),   # counts outside 0 ... S are the nearer end
     (1, 8, 64, 1000, 16, [7], None),
+    (2, 3, 64, 100, 32, [17, 31], [100, 2]),
+    (2, 2, 128, 150, 64, [5, 64], [150, 63]),
+    (1, 3, 64, 260, 128, [127], None),
 ]
 
 
@@ -142,3 +145,38 @@ def test_every_code_and_exponent_is_read_exactly():
     want = bf16(np.clip(np.concatenate([E4M3[codes] * 2.0 ** (e - 127.0) for e in exps]), -2.0 ** 128, 2.0 ** 128))
     for got in (host(k)[0, 0], host(v)[0, 0]):
         assert np.array_equal(got, want, equal_nan=True)
+
+
+def test_strided_rows_and_a_part_of_a_wider_table():
+    """Keys and values as views of one projection's output, results read into views: nothing beside them is touched."""
+    import torch
+    from paper_2604_18616_amd import binding
+    rng = np.random.default_rng(8)
+    B, H, D, S, page = 2, 3, 64, 37, 16
+    table, P = make_table(rng, [S + 9] * B, page)
+    cache = make_cache(rng, P, H, page, D)
+    x = bf16(rng.standard_normal((B, S, 2 * H + 4, D)))
+    buf = bf16_cuda(x)
+    k, v = buf[:, :, 4:4 + H].transpose(1, 2), buf[:, :, 4 + H:].transpose(1, 2)
+    xt = x.transpose(0, 2, 1, 3)
+    want = [t.copy() for t in cache]
+    write_reference(want, xt[:, 4:4 + H], xt[:, 4 + H:], table, [9, 0], [S, 20])
+    dev, tab = to_cuda(cache, table)
+    wide = torch.full((B, table.shape[1] + 5), -1, dtype=torch.int32, device="cuda")
+    wide[:, 2:2 + table.shape[1]] = tab
+    part = wide[:, 2:2 + table.shape[1]]
+    assert binding.kv_fp8_write(dev, k, v, part, whole([9, 0]), whole([S, 20])) is dev
+    torch.cuda.synchronize()
+    check([host(t) for t in dev], want)
+    room = torch.full((B, S + 2, 2 * H, D + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    ko, vo = (room[:, 1:1 + S, h:h + H, :D].transpose(1, 2) for h in (0, H))
+    got = binding.kv_fp8_read(dev, part, whole([S + 9, 20]), S, first=3, k=ko, v=vo)
+    torch.cuda.synchronize()
+    assert got[0] is ko and got[1] is vo
+    for b, n in enumerate((S + 9, 20)):
+        for h in range(H):
+            for out, ref in zip((host(ko)[b, h], host(vo)[b, h]), gather_reference(want, table, b, h, n)):
+                m = min(S, n - 3)
+                assert np.array_equal(out[:m], ref[3:3 + m]) and not out[m:].any()
+    ko.fill_(7.0), vo.fill_(7.0)
+    assert (room == 7.0).all()

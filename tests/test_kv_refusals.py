@@ -83,9 +83,9 @@ def test_read_refuses(lib):
 
 def test_attention_refuses(lib):
     def a(q=A, c=None, table=A, pitch=8, width=8, lens=A, q_lens=None, o=A, lse=A, B=1, Hq=4, Sq=2, qs=GOOD, os_=GOOD, causal=1, window=0, sinks=0,
-          scale=0.1, max_len=0, ws=None, wsb=0, splits=0, **kw):
+          scale=0.1, max_len=0, ws=None, wsb=0, splits=0, wg_rows=0, **kw):
         return lib.attn_kv_fp8(q, c or cache(**kw), table, pitch, width, lens, q_lens, o, lse, B, Hq, Sq, qs, os_, causal, window, sinks, scale, max_len,
-                               ws, wsb, splits, None)
+                               ws, wsb, splits, wg_rows, None)
 
     for kw, code in BAD_CACHES:
         assert a(**kw) == code, kw
@@ -94,7 +94,7 @@ def test_attention_refuses(lib):
     for kw in (dict(B=0), dict(Hq=0), dict(Hq=5), dict(Sq=0), dict(window=-1), dict(sinks=-1), dict(max_len=-1), dict(Sq=1 << 28), dict(B=1 << 20, Sq=1 << 20),
                dict(width=-1), dict(qs=L3(0, 0, 64)), dict(os_=L3(0, -8, 128))):
         assert a(**kw) == -2, kw
-    for kw in (dict(splits=-1), dict(splits=257)):
+    for kw in (dict(splits=-1), dict(splits=257), dict(wg_rows=32), dict(wg_rows=-16)):
         assert a(**kw) == -3, kw
     for kw in (dict(q=A + 2), dict(o=A + 8), dict(lse=A + 2), dict(lens=A + 1), dict(q_lens=A + 2), dict(ws=A + 8, wsb=1 << 20), dict(qs=L3(0, 4, 128))):
         assert a(**kw) == -4, kw

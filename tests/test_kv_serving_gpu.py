@@ -212,3 +212,32 @@ def test_the_same_bits_every_time():
         torch.cuda.synchronize()
         for o, lse in results[1:]:
             assert same(o, results[0][0]) and same(lse, results[0][1])
+
+
+@pytest.mark.parametrize("Sq", [1, 150])
+def test_offsets_past_32_bits(Sq):
+    """Pages behind the first 4 GiB of codes: written, attended to and read back as in a small cache."""
+    import torch
+    from paper_2604_18616_amd import binding
+    page, D, H, far = 128, 128, 2, 1 << 17                   # far * H * page * D = 2^32
+    rng = np.random.default_rng(9)
+    order = rng.permutation(8)
+    near_table = torch.from_numpy(order.reshape(2, 4).astype(np.int32)).cuda()
+    near, large = binding.kv_fp8_cache(8, H, page, D), binding.kv_fp8_cache(far + 8, H, page, D)
+    for t in near:
+        t.fill_(0x7F)
+    for t in large:
+        t[far:].fill_(0x7F)
+    x = torch.from_numpy(bf16(rng.standard_normal((2, 450, H, D)))).to(torch.bfloat16).cuda().transpose(1, 2)
+    q = torch.from_numpy(bf16(rng.standard_normal((2, 8, Sq, D)))).to(torch.bfloat16).cuda()
+    lens = torch.tensor([451, 463], dtype=torch.int32, device="cuda")
+    results = []
+    for cache, table in ((near, near_table), (large, near_table + far)):
+        binding.kv_fp8_write(cache, x, 2 * x, table, torch.tensor([1, 13], dtype=torch.int32, device="cuda"))
+        binding.kv_fp8_write(cache, -x[:, :, :20], x[:, :, :20], table, torch.tensor([0, 0], dtype=torch.int32, device="cuda"))
+        results.append([t[-8:].clone() for t in cache] + list(binding.kv_fp8_read(cache, table, lens, 470)) +
+                       [t for rows in (0, 16, 128) for t in binding.attn_kv_fp8(q, cache, table, lens, causal=True, wg_rows=rows)])
+    torch.cuda.synchronize()
+    for a, b in zip(*results):
+        assert same(a, b)
+    assert torch.isfinite(results[0][-2]).all()

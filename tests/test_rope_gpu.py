@@ -126,3 +126,39 @@ def test_long_context_frequencies():
     assert np.allclose(got, inv * (keep + (1 - keep) / factor), rtol=1e-14, atol=0)
     assert got[0] == 1.0 and np.isclose(got[-1], inv[-1] / factor, rtol=1e-14)
     assert np.allclose(binding.rope_frequencies(R, base, factor).cpu().numpy(), inv / factor, rtol=1e-14, atol=0)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_many_tokens(interleaved):
+    """Enough of them for a thread to walk several heads, numbers of heads that do not divide."""
+    import torch
+    from paper_2604_18616_amd import binding
+    rng = np.random.default_rng(3)
+    B, S, Hq, Hk, D, R = 1, 4500, 33, 7, 128, 96
+    q, k = (bf16(rng.standard_normal((B, H, S, D), dtype=np.float32)) for H in (Hq, Hk))
+    positions = rng.integers(0, 100000, (B, S)).astype(np.int32)
+    inv = binding.rope_frequencies(R)
+    got = binding.rope_bf16(bf16_cuda(q), torch.from_numpy(positions).cuda(), inv, k=bf16_cuda(k), interleaved=interleaved)
+    torch.cuda.synchronize()
+    for g, x in zip(got, (q, k)):
+        check(g, reference(x, positions, inv.cpu().numpy(), interleaved, False, 1.0))
+
+
+def test_outputs_given_and_not_dense():
+    import torch
+    from paper_2604_18616_amd import binding
+    rng = np.random.default_rng(4)
+    q, k = bf16(rng.standard_normal((2, 3, 5, 64))), bf16(rng.standard_normal((1, 2, 5, 64)))
+    room = torch.full((2, 7, 6, 72), 7.0, dtype=torch.bfloat16, device="cuda")
+    qo, ko = room[:, 1:6, :3, :64].transpose(1, 2), room[:, 1:6, 3:5, :64].transpose(1, 2)
+    kd = bf16_cuda(k).expand(2, 2, 5, 64)                    # one sequence's keys for both
+    positions, inv = np.array([[3, 1, 4, 1, 5], [9, 2, 6, 5, 3]], dtype=np.int32), binding.rope_frequencies(48)
+    got = binding.rope_bf16(bf16_cuda(q), torch.from_numpy(positions).cuda(), inv, k=kd, q_out=qo, k_out=ko)
+    own = binding.rope_bf16(bf16_cuda(q), torch.from_numpy(positions).cuda(), inv, k=kd)
+    torch.cuda.synchronize()
+    assert got[0] is qo and got[1] is ko
+    for pair in (got, own):
+        check(pair[0], reference(q, positions, inv.cpu().numpy(), False, False, 1.0))
+        check(pair[1], reference(np.broadcast_to(k, (2, 2, 5, 64)), positions, inv.cpu().numpy(), False, False, 1.0))
+    qo.fill_(7.0), ko.fill_(7.0)
+    assert (room == 7.0).all()
