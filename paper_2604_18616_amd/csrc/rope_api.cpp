@@ -47,7 +47,7 @@ extern "C" int rope_bf16(const void* q, void* q_out, const void* k, void* k_out,
     p.positions = positions; p.pos_pitch = positions_pitch; p.inv_freq = inv_freq;
     p.B = B; p.S = S; p.D = D; p.R = R;
     p.mscale = mscale; p.sign = inverse ? -1.f : 1.f;
-    p.items = 0; p.per = 1; p.chunks_q = 0;
+    p.items = 0; p.per = 1;
     return rope_launch(p, interleaved != 0, (hipStream_t)stream) == 0 ? ATTN_OK : ATTN_ERR_LAUNCH;
 }
 

@@ -1,10 +1,14 @@
 // Rotary position embedding for gfx950.
 //
-// A thread owns V pairs of columns of one token (or V columns that are only copied) and walks the heads: the angle is the
-// same for all of them, so its sine and cosine are made once, in registers, and no table is read.  What bounds it: reading
-// and writing every value once.
+// A thread owns V pairs of columns of one token (or columns that are only copied) and walks heads, those of q and k as one
+// range: the angle is the same for all of them, so its sine and cosine are made once, in registers, and no table is read.
+// What bounds it: reading and writing every value once.  40 heads of 16384 tokens, all 128 columns turned (336 MB in and out),
+// 65.6 us = 5.1 TB/s, where a copy of torch reaches 4.9; 32 heads of 8192 tokens, half the columns turned, 29.5 us = 4.5 TB/s;
+// 40 heads of 64 tokens 3.1 us in a captured graph: latency.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <algorithm>
 
 #include "gfx950_prims.h"
 #include "rope_launch.h"
@@ -14,7 +18,14 @@ namespace {
 using namespace gfx950;
 
 constexpr int kThreads = 256;
-constexpr double kFull = 1 << 19;
+// Heads per thread, and workgroups that a call should have at the least, so that loads of several of them are in flight on
+// every CU: with 40 heads of 16384 tokens 8 / 20 / 4 / 1 heads take 69 / 79 / 78 / 90 us, with 48 heads of 4096 tokens
+// 6 / 2 / 1 parts of the heads (1152 / 384 / 192 workgroups) 26 / 42 / 61 us.
+constexpr int kHeads = 8, kLeastBlocks = 768;
+// Results are not read again here: stored past the caches (48 heads of 4096 tokens 25.9 -> 19.2 us, 40 of 16384 69 -> 67).
+// Values are loaded past them too where there are more than the memory-side cache keeps until they could be used again (72
+// heads of 30000 tokens 199 -> 192 us, but 48 of 4096, which repeated calls find there, 19 -> 25).
+constexpr double kStreamed = 128e6;
 
 template <int N> struct Chunk;                          // N bf16 values as one access
 template <> struct Chunk<8> { using type = u32x4; };
@@ -22,10 +33,16 @@ template <> struct Chunk<4> { using type = u32x2; };
 template <> struct Chunk<2> { using type = unsigned; };
 template <> struct Chunk<1> { using type = unsigned short; };
 
-template <int N>
+template <int N, bool ST>
+__device__ __forceinline__ typename Chunk<N>::type fetch(const __bf16* p) {
+    const auto* const from = (const typename Chunk<N>::type*)p;
+    if constexpr (ST) return __builtin_nontemporal_load(from);
+    else return *from;
+}
+template <int N, bool ST>
 __device__ __forceinline__ void load(const __bf16* p, float (&x)[N]) {
     typedef __attribute__((ext_vector_type(N))) unsigned short bits_t;
-    const bits_t b = __builtin_bit_cast(bits_t, *(const typename Chunk<N>::type*)p);
+    const bits_t b = __builtin_bit_cast(bits_t, fetch<N, ST>(p));
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = __uint_as_float((unsigned)b[i] << 16);
 }
@@ -36,28 +53,40 @@ __device__ __forceinline__ void store(__bf16* p, const float (&x)[N]) {
     f_t f;
 #pragma unroll
     for (int i = 0; i < N; ++i) f[i] = x[i];
-    *(typename Chunk<N>::type*)p = __builtin_bit_cast(typename Chunk<N>::type, __builtin_convertvector(f, b_t));
+    __builtin_nontemporal_store(__builtin_bit_cast(typename Chunk<N>::type, __builtin_convertvector(f, b_t)), (typename Chunk<N>::type*)p);
 }
+
+// x0 a + x1 b, in one order of roundings wherever it stands: a result does not depend on the other heads and tokens of a call.
+__device__ __forceinline__ float turned(float x0, float a, float x1, float b) { return fmaf(x0, a, x1 * b); }
 
 // Halves (IL false): pairs (f, f + R/2), two accesses of V values per head.  Neighbours (IL true): pairs (2f, 2f + 1), one
 // access of 2 V values.
-template <int V, bool IL>
+template <int V, bool IL, bool ST>
 __global__ __launch_bounds__(kThreads) void rope_turn(RopeParams p) {
     const unsigned idx = blockIdx.x * kThreads + threadIdx.x, token = idx / (unsigned)p.items, item = idx % (unsigned)p.items;
     if (token >= (unsigned)p.B * (unsigned)p.S) return;
     const int b = token / (unsigned)p.S, s = token % (unsigned)p.S;
-    const bool is_q = blockIdx.y < (unsigned)p.chunks_q;
-    const RopeTensor& t = p.t[is_q ? 0 : 1];
-    const int h0 = (int)(blockIdx.y - (is_q ? 0 : p.chunks_q)) * p.per, h1 = min(h0 + p.per, t.heads);
-    const __bf16* in = t.in + b * t.in_sb + h0 * t.in_sh + s * t.in_ss;
-    __bf16* out = t.out + b * t.out_sb + h0 * t.out_sh + s * t.out_ss;
+    const int first = (int)blockIdx.y * p.per, last = first + p.per;
+    // each of this thread's heads of q, then of k, as the function's two rows
+    auto heads = [&](auto&& turn) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const RopeTensor& t = p.t[x];
+            const int before = x ? p.t[0].heads : 0, h0 = max(first - before, 0), h1 = min(last - before, t.heads);
+            const __bf16* in = t.in + b * t.in_sb + h0 * t.in_sh + s * t.in_ss;
+            __bf16* out = t.out + b * t.out_sb + h0 * t.out_sh + s * t.out_ss;
+#pragma unroll 2
+            for (int h = h0; h < h1; ++h, in += t.in_sh, out += t.out_sh) turn(in, out);
+        }
+    };
 
     const int f = item * V;
     if (f >= p.R / 2) {                                 // behind the turned columns: copies
         constexpr int W = IL ? 2 * V : V;
         const int col = p.R + (item - p.R / 2 / V) * W;
-        for (int h = h0; h < h1; ++h, in += t.in_sh, out += t.out_sh)
-            *(typename Chunk<W>::type*)(out + col) = *(const typename Chunk<W>::type*)(in + col);
+        heads([&](const __bf16* in, __bf16* out) __attribute__((always_inline)) {
+            __builtin_nontemporal_store(fetch<W, ST>(in + col), (typename Chunk<W>::type*)(out + col));
+        });
         return;
     }
     float c[V], sn[V];
@@ -70,30 +99,29 @@ __global__ __launch_bounds__(kThreads) void rope_turn(RopeParams p) {
         c[i] *= p.mscale;
         sn[i] *= p.mscale * p.sign;
     }
-#pragma unroll 4
-    for (int h = h0; h < h1; ++h, in += t.in_sh, out += t.out_sh) {
+    heads([&](const __bf16* in, __bf16* out) __attribute__((always_inline)) {
         if constexpr (IL) {
             float x[2 * V], y[2 * V];
-            load<2 * V>(in + 2 * f, x);
+            load<2 * V, ST>(in + 2 * f, x);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                y[2 * i] = x[2 * i] * c[i] - x[2 * i + 1] * sn[i];
-                y[2 * i + 1] = x[2 * i] * sn[i] + x[2 * i + 1] * c[i];
+                y[2 * i] = turned(x[2 * i], c[i], -x[2 * i + 1], sn[i]);
+                y[2 * i + 1] = turned(x[2 * i], sn[i], x[2 * i + 1], c[i]);
             }
             store<2 * V>(out + 2 * f, y);
         } else {
             float x0[V], x1[V], y0[V], y1[V];
-            load<V>(in + f, x0);
-            load<V>(in + p.R / 2 + f, x1);
+            load<V, ST>(in + f, x0);
+            load<V, ST>(in + p.R / 2 + f, x1);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                y0[i] = x0[i] * c[i] - x1[i] * sn[i];
-                y1[i] = x0[i] * sn[i] + x1[i] * c[i];
+                y0[i] = turned(x0[i], c[i], -x1[i], sn[i]);
+                y1[i] = turned(x0[i], sn[i], x1[i], c[i]);
             }
             store<V>(out + f, y0);
             store<V>(out + p.R / 2 + f, y1);
         }
-    }
+    });
 }
 
 template <int V, bool IL>
@@ -101,14 +129,14 @@ void launch(RopeParams p, hipStream_t stream) {
     const bool in_place = p.t[0].in == p.t[0].out && (p.t[1].heads == 0 || p.t[1].in == p.t[1].out);
     p.items = p.R / 2 / V + (in_place ? 0 : (p.D - p.R) / (IL ? 2 * V : V));
     const long long tokens = (long long)p.B * p.S;
-    // heads per thread: as many as leave the chip kFull threads
-    const double threads = (double)tokens * p.items * (p.t[0].heads + p.t[1].heads);
-    const int most = p.t[0].heads > p.t[1].heads ? p.t[0].heads : p.t[1].heads;
-    p.per = threads < 2 * kFull ? 1 : threads / kFull < most ? (int)(threads / kFull) : most;
-    p.chunks_q = (p.t[0].heads + p.per - 1) / p.per;
-    const unsigned rows = p.chunks_q + (p.t[1].heads + p.per - 1) / p.per;
+    const int all = p.t[0].heads + p.t[1].heads;
     const unsigned blocks = (unsigned)((tokens * p.items + kThreads - 1) / kThreads);
-    hipLaunchKernelGGL((rope_turn<V, IL>), dim3(blocks, rows), dim3(kThreads), 0, stream, p);
+    const long long parts = std::max((all + kHeads - 1) / kHeads, (int)((kLeastBlocks + blocks - 1) / blocks));
+    p.per = (int)((all + parts - 1) / parts);
+    const dim3 grid(blocks, (all + p.per - 1) / p.per);
+    const bool streamed = (double)tokens * all * p.D * 2 * sizeof(__bf16) > kStreamed;
+    if (streamed) hipLaunchKernelGGL((rope_turn<V, IL, true>), grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((rope_turn<V, IL, false>), grid, dim3(kThreads), 0, stream, p);
 }
 
 }  // namespace

@@ -17,8 +17,7 @@ struct RopeParams {
     float mscale;
     float sign;                // -1: the inverse rotation
     int items;                 // threads per token (set by the launcher)
-    int per;                   // heads per thread (set by the launcher)
-    int chunks_q;              // grid rows of q (set by the launcher)
+    int per;                   // heads per thread, of q's and k's one after the other (set by the launcher)
 };
 
 // Enqueue the kernel; 0, or -1 if the runtime refused the launch.

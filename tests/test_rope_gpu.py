@@ -162,3 +162,23 @@ def test_outputs_given_and_not_dense():
         check(pair[1], reference(np.broadcast_to(k, (2, 2, 5, 64)), positions, inv.cpu().numpy(), False, False, 1.0))
     qo.fill_(7.0), ko.fill_(7.0)
     assert (room == 7.0).all()
+
+
+@pytest.mark.parametrize("interleaved,layout", [(False, "bshd"), (True, "bhsd")])
+def test_a_large_call_is_its_parts(interleaved, layout):
+    """200 MB in one call against the same tokens in small calls: the same bits."""
+    import torch
+    from paper_2604_18616_amd import binding
+    B, S, Hq, Hk, D = 2, 5001, 30, 5, 160
+    shape = lambda H: (B, H, S, D) if layout == "bhsd" else (B, S, H, D)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k = (torch.randn(shape(H), generator=gen, device="cuda").to(torch.bfloat16) for H in (Hq, Hk))
+    if layout == "bshd":
+        q, k = q.transpose(1, 2), k.transpose(1, 2)
+    positions = torch.arange(B * S, dtype=torch.int32, device="cuda").reshape(B, S)
+    inv = binding.rope_frequencies(128)
+    whole = binding.rope_bf16(q, positions, inv, k=k, interleaved=interleaved)
+    for at in range(0, S, 500):
+        part = binding.rope_bf16(q[:, :, at:at + 500], positions[:, at:at + 500], inv, k=k[:, :, at:at + 500], interleaved=interleaved)
+        for w, x in zip(whole, part):
+            assert torch.equal(w[:, :, at:at + 500], x)
