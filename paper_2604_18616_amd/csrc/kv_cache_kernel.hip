@@ -14,10 +14,6 @@ constexpr int kLeastExp = -100;
 constexpr int kReadRows = 64;        // positions per workgroup of kv_read
 
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }    // -126 <= e <= 127
-__device__ __forceinline__ unsigned char to_e4m3(float x) {
-    return (unsigned char)(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xff);
-}
-__device__ __forceinline__ float from_e4m3(unsigned char c) { return __builtin_amdgcn_cvt_f32_fp8((int)c, 0); }
 
 // The least e >= kLeastExp with amax <= 448 * 2^e = 1.75 * 2^(e + 8).
 __device__ __forceinline__ int exponent_for(float amax) {
@@ -40,6 +36,14 @@ __device__ __forceinline__ u32x2 codes_of(u32x4 w, float f) {
         out[j] = (c & ~odd) | (0x7f7f7f7fu & odd);
     }
     return out;
+}
+// Four codes rounded again to c * f; the NaN codes stay.
+__device__ __forceinline__ unsigned again(unsigned w, float f) {
+    const unsigned nan = ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu;
+    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+    unsigned c = __builtin_amdgcn_cvt_pk_fp8_f32(a[0] * f, a[1] * f, 0, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(b[0] * f, b[1] * f, c, true);
+    return (c & ~nan) | (w & nan);
 }
 // The largest finite |x| of eight values, as the bits of a bf16 (which order as the values do).
 __device__ __forceinline__ unsigned largest(u32x4 w, unsigned m) {
@@ -69,7 +73,8 @@ __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
     const int h = id % (unsigned)p.c.Hkv; id /= (unsigned)p.c.Hkv;
     const int f = id % (unsigned)p.F, b = id / (unsigned)p.F;
 
-    // the unit's tokens: `held` earlier ones of the page, then `fresh` new ones; none where there is nothing to do
+    // the unit's tokens: `held` earlier ones of the page, then `fresh` new ones; none where there is nothing to do.  (The new values
+    // are on their way before it is known whether the page is there: one latency less.)
     int held = 0, fresh = 0, at = -1;
     long long token0 = 0;                                              // of the new ones, the first
     if (b < p.B) {
@@ -80,13 +85,9 @@ __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
         const long long lo = start > base ? start : base, hi = start + n < base + PAGE ? start + n : base + PAGE;
         if (pg >= 0 && pg < p.c.W && lo < hi) {
             at = p.c.table[b * p.c.pitch + pg];
-            if (at >= 0 && at < p.c.P) { held = (int)(lo - base); fresh = (int)(hi - lo); token0 = lo - start; }
+            held = (int)(lo - base); fresh = (int)(hi - lo); token0 = lo - start;
         }
     }
-    if (TPU == 256 && fresh == 0) return;
-    const size_t unit = (size_t)(fresh ? at : 0) * p.c.Hkv + h;
-    unsigned char* const codes = (is_v ? p.c.v : p.c.k) + unit * PAGE * D;
-    unsigned char* const exps = (is_v ? p.c.ve : p.c.ke) + unit;
     const long long row = is_v ? p.v_ss : p.k_ss;
     const __bf16* const src = (is_v ? p.v + b * p.v_sb + h * p.v_sh : p.k + b * p.k_sb + h * p.k_sh) + (token0 - held) * row;   // of token 0 of the page
 
@@ -102,6 +103,11 @@ __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
             if (t >= held && t < held + fresh) x[n][j] = *(const u32x4*)(src + t * row + c * 8);
         }
     }
+    if (at < 0 || at >= p.c.P) fresh = 0;
+    if (TPU == 256 && fresh == 0) return;
+    const size_t unit = (size_t)(fresh ? at : 0) * p.c.Hkv + h;
+    unsigned char* const codes = (is_v ? p.c.v : p.c.k) + unit * PAGE * D;
+    unsigned char* const exps = (is_v ? p.c.ve : p.c.ke) + unit;
     int e_old = fresh ? (int)*exps - 127 : 0;
 #pragma unroll
     for (int n = 0; n < NB; ++n)
@@ -117,12 +123,13 @@ __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
     int e = exponent_for(__uint_as_float(m << 16));
     if (held > 0 && e < e_old) e = e_old;
 
-    // a scale that has grown: the earlier tokens' codes are rounded again
-    if (held > 0 && fresh > 0 && e > e_old) {
-        const float f2 = two_to(max(e_old - e, -126));
-        for (int i = tid; i < held * D; i += TPU) {
-            unsigned char* const c = codes + (is_v ? (i / held) * PAGE + i % held : i);
-            if ((*c & 0x7f) != 0x7f) *c = to_e4m3(from_e4m3(*c) * f2);
+    // a scale that has grown: the earlier tokens' codes are rounded again, those of V where their pieces are written
+    const bool grown = held > 0 && fresh > 0 && e > e_old;
+    const float f2 = grown ? two_to(max(e_old - e, -126)) : 1.f;
+    if (grown && !is_v) {
+        for (int i = tid; i < held * (D / 16); i += TPU) {
+            u32x4* const c = (u32x4*)codes + i;
+            *c = u32x4{again((*c)[0], f2), again((*c)[1], f2), again((*c)[2], f2), again((*c)[3], f2)};
         }
     }
     const float f1 = two_to(-e);
@@ -130,6 +137,7 @@ __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
     for (int n = 0; n < NB; ++n) {
         const int blk = n * TPU + tid, q = blk / CPR, c = blk % CPR;
         if (BLOCKS % TPU != 0 && blk >= BLOCKS) break;
+        if (4 * q + 4 <= held || 4 * q >= held + fresh) continue;      // (no new token: what lies in LDS there is not used)
         u32x2 w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = codes_of(x[n][j], f1);
@@ -155,11 +163,21 @@ __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
         }
         for (int i = tid; i < D * (PAGE / 16); i += TPU) {
             const int d = i / (PAGE / 16), t = i % (PAGE / 16) * 16;
-            if (t + 16 <= held || t >= held + fresh) continue;
+            if (t >= held + fresh || (t + 16 <= held && !grown)) continue;
             u32x4 w;
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = s_page[sub][d * PITCH + t / 4 + j];
-            if (t >= held && t + 16 <= held + fresh) *(u32x4*)(codes + d * PAGE + t) = w;
+            u32x4* const piece = (u32x4*)(codes + d * PAGE + t);
+            if (grown && t < held) {                                   // earlier tokens, new ones, and what lies behind them
+                const u32x4 old = *piece;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    auto bytes = [](int n) __attribute__((always_inline)) { n = min(max(n, 0), 4); return n == 4 ? ~0u : (1u << (8 * n)) - 1; };
+                    const unsigned was = bytes(held - t - 4 * j), now = bytes(held + fresh - t - 4 * j) & ~was;
+                    w[j] = (again(old[j], f2) & was) | (w[j] & now) | (old[j] & ~(was | now));
+                }
+                *piece = w;
+            } else if (t >= held && t + 16 <= held + fresh) *piece = w;
             else {
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
