@@ -382,7 +382,7 @@ template <int PIECES> __device__ __forceinline__ constexpr int piece_offset(int 
 
 constexpr int kTileWaves = 4;
 template <int D>
-__global__ __launch_bounds__(kTileWaves * 64, 2) void attn_kv_tiles(KvAttnParams p) {
+__global__ __launch_bounds__(kTileWaves * 64, D == 64 ? 3 : 2) void attn_kv_tiles(KvAttnParams p) {
     constexpr int KS = D / 16, DB = D / 32, KP = D / 8;
     constexpr int NC = D / 64;                            // 16-code pieces per thread, tile and matrix
     constexpr int STAGE = 2 * kTile * D * 2;              // bytes of a K and a V tile
@@ -751,6 +751,47 @@ __global__ __launch_bounds__(256) void attn_kv_combine(KvAttnParams p) {
     }
 }
 
+// The same for up to kJoinParts parts: a wavefront per row, all its loads in flight at once, no LDS.
+constexpr int kJoinParts = 16;
+template <int D>
+__global__ __launch_bounds__(256) void attn_kv_join(KvAttnParams p) {
+    constexpr int QPR = D / 4, NS = 64 / QPR, NL = kJoinParts / NS;
+    const int lane = threadIdx.x & 63, sl = lane / QPR, d = lane % QPR * 4, S = p.splits;
+    const unsigned rowi = blockIdx.x * 4 + (threadIdx.x >> 6), bh = rowi / (unsigned)p.Sq;
+    if (rowi >= (unsigned)p.B * p.Hq * p.Sq) return;
+    const int i = rowi - bh * p.Sq, b = bh / (unsigned)p.Hq, hq = bh - b * p.Hq;
+    const f32x2 ml = lane < S ? *(const f32x2*)(p.ml + 2 * ((size_t)rowi * S + lane)) : f32x2{-INFINITY, 0.f};
+    f32x4 v[NL];
+#pragma unroll
+    for (int n = 0; n < NL; ++n) {
+        const int s = n * NS + sl;
+        v[n] = s < S ? *(const f32x4*)(p.part + ((size_t)rowi * S + s) * D + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    float m = ml[0];
+#pragma unroll
+    for (int x = kJoinParts / 2; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
+    const float w = ml[0] == -INFINITY ? 0.f : exp2_hw((ml[0] - m) * p.scale_log2);
+    float l = ml[1] * w;
+#pragma unroll
+    for (int x = kJoinParts / 2; x > 0; x >>= 1) l += __shfl_xor(l, x);
+    m = __shfl(m, 0); l = __shfl(l, 0);                                               // (the lanes from kJoinParts on had no part)
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < NL; ++n) {
+        const float ws = __shfl(w, n * NS + sl), ms = __shfl(ml[0], n * NS + sl);
+        if (ms != -INFINITY) acc += v[n] * ws;                                        // (a part without keys is not written)
+    }
+#pragma unroll
+    for (int x = QPR; x < 64; x <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], x);
+    const bool none = l == 0.f;
+    const float inv = none ? 0.f : 1.f / l;
+    const u32x2 out = {pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+    if (sl == 0) *(u32x2*)(p.o + b * p.o_sb + hq * p.o_sh + (long long)i * p.o_ss + d) = none ? u32x2{0, 0} : out;
+    if (lane == 0 && p.lse) p.lse[rowi] = none ? -INFINITY : m * p.scale + logf(l);
+}
+
 }  // namespace
 
 // Time of a call in microseconds, from what was measured on shapes of 1 to 128 sequences, 300 to 64000 keys, 1 to 256 packed rows.
@@ -759,21 +800,25 @@ __global__ __launch_bounds__(256) void attn_kv_combine(KvAttnParams p) {
 // times that where both are alike.  Parts cost a second kernel and their traffic.
 static double estimate(const KvAttnPlan& plan, long long pairs, long long rows, int tiles, int D) {
     const bool rows16 = plan.rows == kBlock, wide = D == 128;
-    const long long n = pairs * plan.row_wgs * plan.splits, slots = rows16 && plan.waves == 8 ? 256 : rows16 && !wide ? 768 : 512;
+    const long long n = pairs * plan.row_wgs * plan.splits, slots = rows16 && plan.waves == 8 ? 256 : wide ? 512 : 768;
     const double start = rows16 ? (plan.waves == 8 ? (wide ? 6.6 : 5.6) : wide ? 5.2 : 4.8) : 6.5;
-    // a step is a tile of every wavefront (rows) or of the workgroup: with one workgroup on a CU, and with the CU full
+    // a step is a tile of every wavefront (rows) or of the workgroup: with one workgroup on a CU, with two, and with the CU full
     const double alone = rows16 ? (plan.waves == 8 ? (wide ? 2.5 : 1.0) : wide ? 1.3 : 0.72) : wide ? 1.21 : 0.95;
-    const double full = rows16 ? (plan.waves == 8 ? alone : wide ? 2.1 : 1.6) : wide ? 2.07 : 1.36;
+    const double full = rows16 ? (plan.waves == 8 ? alone : wide ? 2.1 : 1.6) : wide ? 2.07 : 1.87;
+    const double two = rows16 || wide ? full : 1.33;
     const int per = (tiles + plan.splits - 1) / plan.splits, steps = rows16 ? (per + plan.waves - 1) / plan.waves : per;
     const double bytes = (double)tiles / plan.splits * kTile * D * 2 / plan.row_wgs;          // of a workgroup, its row blocks sharing an L2
     auto round = [&](long long wgs) {
-        const double work = steps * (wgs <= 256 ? alone : full), hbm = wgs * bytes / 6.2e6;
+        const double work = steps * (wgs <= 256 ? alone : wgs <= 512 ? two : full), hbm = wgs * bytes / 6.2e6;
         const double both = sqrt(work * work + hbm * hbm) * (rows16 && plan.waves == 8 ? 0.9 : 1.0);
         return start + (both > work ? (both > hbm ? both : hbm) : work);
     };
     double t = (double)(n / slots) * (n >= slots ? round(slots) : 0.0);
     if (n % slots) t += round(n % slots);
-    if (plan.splits > 1) t += 4.2 + rows * 0.0008 + (double)rows * plan.splits * (D + 2) * 1.6e-6;
+    if (plan.splits > 1) {
+        const double each = rows * (plan.splits <= kJoinParts ? 0.00036 : 0.0014), parts = (double)rows * plan.splits * (D + 2) * 4 / 5.5e6;
+        t += 4.0 + (each > parts ? each : parts) + 0.8 * parts;
+    }
     return t;
 }
 
@@ -823,13 +868,12 @@ int attn_kv_launch(KvAttnParams p, const KvAttnPlan& plan, hipStream_t stream) {
     if (hipGetLastError() != hipSuccess) return -1;
     if (p.splits > 1) {
         const unsigned rows = (unsigned)p.B * p.Hq * p.Sq;
-        // 32 columns per workgroup where all of them would take more than one batch: 8 rows of 256 parts, call 16.4 -> 13.9 us; 32 rows
-        // of 8 or 64 parts 9.4 / 9.4, 9.8 / 9.5
-        const bool many = p.splits > 8 * (256 / (p.c.D / 4));
-        if (p.c.D == 128 && many) hipLaunchKernelGGL((attn_kv_combine<128, 32>), dim3(rows, 4), dim3(256), 0, stream, p);
-        else if (p.c.D == 128) hipLaunchKernelGGL((attn_kv_combine<128, 128>), dim3(rows), dim3(256), 0, stream, p);
-        else if (many) hipLaunchKernelGGL((attn_kv_combine<64, 32>), dim3(rows, 2), dim3(256), 0, stream, p);
-        else hipLaunchKernelGGL((attn_kv_combine<64, 64>), dim3(rows), dim3(256), 0, stream, p);
+        // a wavefront per row for few parts; 32 columns per workgroup where all of them would take more than one batch: 8 rows of 256
+        // parts, call 16.4 -> 13.9 us; 32 rows of 64 parts 9.4 / 9.5
+        const int D = p.c.D;
+        if (p.splits <= kJoinParts) hipLaunchKernelGGL((D == 128 ? attn_kv_join<128> : attn_kv_join<64>), dim3((rows + 3) / 4), dim3(256), 0, stream, p);
+        else if (p.splits > 8 * (256 / (D / 4))) hipLaunchKernelGGL((D == 128 ? attn_kv_combine<128, 32> : attn_kv_combine<64, 32>), dim3(rows, D / 32), dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL((D == 128 ? attn_kv_combine<128, 128> : attn_kv_combine<64, 64>), dim3(rows), dim3(256), 0, stream, p);
         if (hipGetLastError() != hipSuccess) return -1;
     }
     return 0;
