@@ -11,7 +11,10 @@
 //   * codes become bf16, exactly and times the page's scale, by the conversion instruction; 16 keys lie in one page, so the
 //     scale and the page's address are per lane.
 // The keys are cut over the wavefronts of a workgroup and over `splits` workgroups; the wavefronts are merged through LDS,
-// the workgroups of a row by attn_kv_combine from fp32 parts.
+// the workgroups of a row by attn_kv_join or attn_kv_combine from fp32 parts.
+// What bounds it: reading the codes, or latency.  32 sequences of up to 8191 keys, 8 kv heads of 128: 63 us = 4.4 TB/s; 16 of up to
+// 20000 keys with a window of 4096, 16 heads of 64: 25 us = 5.0 TB/s (a copy reaches 4.9); one of 131071 keys, one kv head: 13.6 us
+// (11 and 4 in the two kernels); one of 2000 keys, 8 kv heads: 10 us (7 and 3.5).  Many rows have a kernel of their own below.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <math.h>
@@ -371,8 +374,15 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
 //
 // Row m of a 32-key block of S^T stands for key m with bits 2 and 3 exchanged: then the eight scores that a lane holds for a
 // step of 16 keys are those of eight consecutive keys, one 16-byte piece of its row of V^T.
+//
+// What bounds it: 2 x 1000 rows of 32 heads of 128 against up to 16301 keys take 380 us, 1010 TFLOP/s (a large matrix product
+// 1366); the matrix units are busy 50 % of that, the vector units 51 %, LDS 38 %: the wavefronts' turns at them overlap in part.
+// Two workgroups on a CU (three for D = 64, which its 169 registers just miss without being asked: 4 x 1500 rows against 8000 keys
+// 238 -> 183 us) measured better than one of eight wavefronts; codes kept as they are in LDS and decoded at every read 554 us;
+// a wavefront's priority raised around its matrix instructions 408 to 422; the first 32 keys' probabilities made while the other 32
+// keys' scores are 406.
 // ---------------------------------------------------------------------------------------------------------------------
-constexpr int kTileRows = 32;
+constexpr int kTileRows = 32, kTileWaves = 4;
 __device__ __forceinline__ constexpr int key_of_row(int m) { return (m & 0x13) | ((m >> 1) & 4) | ((m << 1) & 8); }
 // Rows of K (2 D bytes) and of V^T (128 bytes) in pieces of 16 bytes, their places exchanged so that 16 consecutive rows' reads of
 // one piece hit all banks once (rows of 128 bytes: two of them per turn of the banks).
@@ -380,7 +390,6 @@ template <int PIECES> __device__ __forceinline__ constexpr int piece_offset(int 
     return row * PIECES * 16 + ((piece ^ (PIECES == 16 ? row & 15 : (row >> 1) & 7)) << 4);
 }
 
-constexpr int kTileWaves = 4;
 template <int D>
 __global__ __launch_bounds__(kTileWaves * 64, D == 64 ? 3 : 2) void attn_kv_tiles(KvAttnParams p) {
     constexpr int KS = D / 16, DB = D / 32, KP = D / 8;
@@ -751,7 +760,8 @@ __global__ __launch_bounds__(256) void attn_kv_combine(KvAttnParams p) {
     }
 }
 
-// The same for up to kJoinParts parts: a wavefront per row, all its loads in flight at once, no LDS.
+// The same for up to kJoinParts parts: a wavefront per row, all its loads in flight at once, no LDS.  65536 rows of 4 parts,
+// D = 128: 95 us by a workgroup per row, 29 so.
 constexpr int kJoinParts = 16;
 template <int D>
 __global__ __launch_bounds__(256) void attn_kv_join(KvAttnParams p) {
@@ -868,8 +878,8 @@ int attn_kv_launch(KvAttnParams p, const KvAttnPlan& plan, hipStream_t stream) {
     if (hipGetLastError() != hipSuccess) return -1;
     if (p.splits > 1) {
         const unsigned rows = (unsigned)p.B * p.Hq * p.Sq;
-        // a wavefront per row for few parts; 32 columns per workgroup where all of them would take more than one batch: 8 rows of 256
-        // parts, call 16.4 -> 13.9 us; 32 rows of 64 parts 9.4 / 9.5
+        // 32 columns per workgroup where all of them would take more than one batch of loads: 8 rows of 256 parts, call 16.4 -> 13.9
+        // us; 32 rows of 64 parts, one batch, 9.4 and 9.5
         const int D = p.c.D;
         if (p.splits <= kJoinParts) hipLaunchKernelGGL((D == 128 ? attn_kv_join<128> : attn_kv_join<64>), dim3((rows + 3) / 4), dim3(256), 0, stream, p);
         else if (p.splits > 8 * (256 / (D / 4))) hipLaunchKernelGGL((D == 128 ? attn_kv_combine<128, 32> : attn_kv_combine<64, 32>), dim3(rows, D / 32), dim3(256), 0, stream, p);
