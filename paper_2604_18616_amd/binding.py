@@ -260,7 +260,7 @@ def attn_fwd(q, k, v, o=None, lse=None, causal=False, scale=None, stream=None):
     if ws is not None:
         rc = lib.attn_fwd_workspace(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
                                     B, Hq, Hkv, Sq, Sk, D, _Int64x3(*qst[:3]), _Int64x3(*kst[:3]), _Int64x3(*vst[:3]), _Int64x3(*ost[:3]),
-                                    causal, scale, ws.data_ptr(), need, 0 if wg_rows else need // (4 * B * Hq * Sq * (D + 2)), int(wg_rows), stream)
+                                    causal, scale, ws.data_ptr(), need, need // (4 * B * Hq * Sq * (D + 2)), stream)
     elif q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and o.is_contiguous():
         rc = lib.attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
                           B, Hq, Hkv, Sq, Sk, D, causal, scale, stream)
