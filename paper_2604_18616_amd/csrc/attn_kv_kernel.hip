@@ -9,7 +9,8 @@
 //   * row m of key block t of a tile stands for key 16 (m / 4) + 4 t + m % 4, so that after four blocks lane group l / 16
 //     holds the scores of 16 consecutive keys: the same 16 keys whose codes of one d are one 16-byte load of the transposed V;
 //   * codes become bf16, exactly and times the page's scale, by the conversion instruction; 16 keys lie in one page, so the
-//     scale and the page's address are per lane.
+//     scale and the page's address are per lane.  The probabilities are rounded to bf16, which the matrix instruction wants of
+//     both operands; their sum is that of the unrounded ones.
 // The keys are cut over the wavefronts of a workgroup and over `splits` workgroups; the wavefronts are merged through LDS,
 // the workgroups of a row by attn_kv_join or attn_kv_combine from fp32 parts.
 // What bounds it: reading the codes, or latency.  32 sequences of up to 8191 keys, 8 kv heads of 128: 63 us = 4.4 TB/s; 16 of up to
