@@ -92,7 +92,7 @@ int kv_fp8_read(const KvFp8Cache *cache, const int *table, long long table_pitch
  * fixed order: results do not vary from run to run.
  * wg_rows, for tuning and for tests that run every shape both ways: query rows (heads of one kv head side by side) per
  * workgroup, 16, 128, or 0 = the library's choice.
- * Supported: Hq a multiple of Hkv, Hq / Hkv * Sq < 2^28, B * Hq * Sq < 2^31 (cut: 2^24); scale finite and > 0; window, sinks >= 0.
+ * Supported: Hq a multiple of Hkv, Hq / Hkv * Sq < 2^28, B * Hq * Sq < 2^31 (cut: 2^24); 0 < scale <= 1e38; window, sinks >= 0.
  * Errors: NULL_PTR, BAD_SHAPE, UNSUPPORTED (D, page, splits, wg_rows), MISALIGNED (q, o, workspace 16 bytes; lse, lens, table 4),
  * BAD_SCALE, LAUNCH.
  */

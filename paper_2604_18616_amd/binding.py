@@ -8,6 +8,7 @@ HIP library is missing or fails, the call raises.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Any, NamedTuple
 
@@ -414,12 +415,20 @@ def _cache_struct(cache):
     return _CacheStruct(k.data_ptr(), v.data_ptr(), ke.data_ptr(), ve.data_ptr(), P, H, page, D), H, D, k.device
 
 
+def _int32(value, name):
+    """A whole number as the C entry points take it: ctypes would cut off what lies above."""
+    value = operator.index(value)
+    if not -1 << 31 <= value < 1 << 31:
+        raise ValueError("%s does not fit 32 bits" % name)
+    return value
+
+
 def _table(table, device):
     """(address, pitch, batch, width) of a page table."""
     import torch
     if table.dtype != torch.int32 or table.dim() != 2 or table.device != device or (table.shape[1] > 1 and table.stride(1) != 1):
         raise ValueError("the page table must be int32 [B, width] with contiguous rows on the cache's device")
-    return table.data_ptr(), table.stride(0), table.shape[0], table.shape[1]
+    return table.data_ptr(), table.stride(0), _int32(table.shape[0], "the batch"), _int32(table.shape[1], "the table's width")
 
 
 def _per_sequence(t, B, device, name):
@@ -437,6 +446,8 @@ def _rows(t, shape, device, name):
     import torch
     if t.dtype != torch.bfloat16 or tuple(t.shape) != tuple(shape) or t.device != device or t.stride(3) != 1:
         raise ValueError("%s must be bfloat16 %s with contiguous rows on one CUDA device" % (name, list(shape)))
+    for size in shape:
+        _int32(size, "a size of " + name)
     return _strides3(t)
 
 
@@ -499,14 +510,17 @@ def kv_fp8_read(cache, table, lens, S, first=0, k=None, v=None, stream=None):
     import torch
     struct, H, D, device = _cache_struct(cache)
     at, pitch, B, width = _table(table, device)
-    shape = (B, H, int(S), D)
+    S, first = _int32(S, "S"), _int32(first, "first")
+    if S < 1:
+        raise ValueError("S must be at least 1")
+    shape = (B, H, S, D)
     k = torch.empty(shape, dtype=torch.bfloat16, device=device) if k is None else k
     v = torch.empty(shape, dtype=torch.bfloat16, device=device) if v is None else v
     ks, vs = (_rows(t, shape, device, name) for t, name in ((k, "k"), (v, "v")))
     stream, _ = _streams(k, stream)
     lens = _per_sequence(lens, B, device, "lens")
     with _on(device):
-        rc = load_library().kv_fp8_read(ctypes.byref(struct), at, pitch, width, lens, k.data_ptr(), v.data_ptr(), ks, vs, B, int(S), int(first), stream)
+        rc = load_library().kv_fp8_read(ctypes.byref(struct), at, pitch, width, lens, k.data_ptr(), v.data_ptr(), ks, vs, B, S, first, stream)
     if rc != 0:
         raise AttnError(rc, strerror(rc))
     return k, v
@@ -539,7 +553,7 @@ def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=Fal
     elif lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, Sq) or not lse.is_contiguous() or lse.device != device:
         raise ValueError("lse must be a contiguous float32 tensor of shape [B, Hq, Sq] on q's device")
     scale = float(D) ** -0.5 if scale is None else float(scale)
-    window, sinks, max_len = int(window), int(sinks), int(max_len)
+    window, sinks, max_len, wg_rows = (_int32(n, name) for n, name in ((window, "window"), (sinks, "sinks"), (max_len, "max_len"), (wg_rows, "wg_rows")))
     lens, q_lens = _per_sequence(lens, B, device, "lens"), _per_sequence(q_lens, B, device, "q_lens")
     stream, own = _streams(q, stream)
     lib = load_library()
@@ -550,7 +564,7 @@ def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=Fal
     with _on(device):
         rc = lib.attn_kv_fp8(q.data_ptr(), ctypes.byref(struct), at, pitch, width, lens, q_lens, o.data_ptr(), lse.data_ptr(), B, Hq, Sq, qs, os_,
                              1 if causal else 0, window, sinks, scale, max_len, None if ws is None else ws.data_ptr(), 0 if ws is None else need,
-                             1 if ws is None else 0 if wg_rows else need // (4 * B * Hq * Sq * (D + 2)), int(wg_rows), stream)
+                             1 if ws is None else 0 if wg_rows else need // (4 * B * Hq * Sq * (D + 2)), wg_rows, stream)
     if rc != 0:
         raise AttnError(rc, strerror(rc))
     return o, lse

@@ -106,7 +106,7 @@ extern "C" int attn_kv_fp8(const void* q, const KvFp8Cache* cache, const int* ta
     if (((uintptr_t)lse | (uintptr_t)lens | (uintptr_t)q_lens) & 3u) return ATTN_ERR_MISALIGNED;
     if (int rc = check_strides(qs, p.c.D)) return rc;
     if (int rc = check_strides(os, p.c.D)) return rc;
-    if (!(scale > 0.0f) || isinf(scale)) return ATTN_ERR_BAD_SCALE;   // rejects NaN, <= 0, inf
+    if (!(scale > 0.0f) || scale > 1e38f) return ATTN_ERR_BAD_SCALE;   // rejects NaN, <= 0, and what the factor of base 2 would make infinite
 
     p.q = (const __bf16*)q; p.o = (__bf16*)o; p.lse = lse;
     p.q_sb = qs[0]; p.q_sh = qs[1]; p.q_ss = qs[2];

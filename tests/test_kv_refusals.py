@@ -98,7 +98,7 @@ def test_attention_refuses(lib):
         assert a(**kw) == -3, kw
     for kw in (dict(q=A + 2), dict(o=A + 8), dict(lse=A + 2), dict(lens=A + 1), dict(q_lens=A + 2), dict(ws=A + 8, wsb=1 << 20), dict(qs=L3(0, 4, 128))):
         assert a(**kw) == -4, kw
-    for scale in (0.0, -1.0, math.nan, math.inf):
+    for scale in (0.0, -1.0, math.nan, math.inf, 2e38):
         assert a(scale=scale) == -5
 
 

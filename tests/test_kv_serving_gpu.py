@@ -241,3 +241,22 @@ def test_offsets_past_32_bits(Sq):
     for a, b in zip(*results):
         assert same(a, b)
     assert torch.isfinite(results[0][-2]).all()
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    """No number is cut to its lower half."""
+    import torch
+    from paper_2604_18616_amd import binding
+    layer = Layer(7, 1, 4, 2, 64, 16, 64)
+    q, n = torch.zeros((1, 4, 1, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    far = (1 << 32) + 5
+    for _ in modes():
+        for kw in (dict(window=far), dict(sinks=far), dict(max_len=far), dict(window=-far), dict(wg_rows=(1 << 32) + 16)):
+            with pytest.raises(ValueError, match="32 bits"):
+                binding.attn_kv_fp8(q, layer.cache, layer.tab, n, **kw)
+        for S, first in ((far, 0), (4, far)):
+            with pytest.raises(ValueError, match="32 bits"):
+                binding.kv_fp8_read(layer.cache, layer.tab, n, S, first=first)
+        for kw in (dict(window=2.5), dict(sinks="4")):
+            with pytest.raises(TypeError):
+                binding.attn_kv_fp8(q, layer.cache, layer.tab, n, **kw)
