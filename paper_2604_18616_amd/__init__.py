@@ -13,7 +13,8 @@ def __getattr__(name):
     if name in ("attn_fwd", "gemm_bf16", "moe_ffn_fp8", "moe_workspace_bytes", "load_library", "attn_fwd_flops", "rope_bf16", "rope_frequencies",
                 "KvFp8Cache", "kv_fp8_cache", "kv_fp8_write", "kv_fp8_read", "attn_kv_fp8", "strerror", "version", "AttnError"):
         from . import binding
-        return getattr(binding, name)
+        value = globals()[name] = getattr(binding, name)            # (the next access does not come here: 1 us of a small call)
+        return value
     if name == "build_library":
         from .build import build_library
         return build_library
