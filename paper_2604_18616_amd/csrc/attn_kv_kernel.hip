@@ -381,7 +381,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
 // Two workgroups on a CU (three for D = 64, which its 169 registers just miss without being asked: 4 x 1500 rows against 8000 keys
 // 238 -> 183 us) measured better than one of eight wavefronts; codes kept as they are in LDS and decoded at every read 554 us;
 // a wavefront's priority raised around its matrix instructions 408 to 422; the first 32 keys' probabilities made while the other 32
-// keys' scores are 406; 64 rows per wavefront, one wavefront per SIMD, 746.
+// keys' scores are 406; 64 rows per wavefront, one wavefront per SIMD, 746; 256 rows per workgroup in two groups half a tile
+// apart 454, though 477 for two sequences of equal length, which take 521 here (then against the power limit).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int kTileRows = 32, kTileWaves = 4;
 __device__ __forceinline__ constexpr int key_of_row(int m) { return (m & 0x13) | ((m >> 1) & 4) | ((m << 1) & 8); }

@@ -62,7 +62,7 @@ __device__ __forceinline__ unsigned largest(u32x4 w, unsigned m) {
 // tokens x 8 values, once, keeps them while the page's maximum is found, and packs the codes of V by four tokens: the transposed
 // page is put together in LDS and leaves in pieces of 16 tokens.  4 prompts of up to 4096 tokens, 8 heads of 128, pages of 64:
 // 16.2 us = 3.9 TB/s (37 us with a second pass over the values and single bytes of V); one token of 64 sequences, pages of 16 / 64
-// / 128: 6.7 / 9.5 / 12.4 us (every column's byte of V lies in another line), 7.4 / 10.2 / 14.7 where scales grow.
+// / 128: 7.1 / 9.5 / 12.4 us between two events (every column's byte of V lies in another line), 7.4 / 10.2 / 14.7 where scales grow.
 template <int D, int PAGE>
 __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
     constexpr int TPU = PAGE <= 32 ? 64 : 256, UNITS = kThreads / TPU;

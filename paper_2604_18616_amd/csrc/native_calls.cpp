@@ -2,7 +2,7 @@
 // stream, results allocated here) without Python's share of the work: checking the tensors, allocating the results and
 // marshalling two dozen arguments takes longer there than a small kernel runs.  Host time per call on the machine measured,
 // Python against this: attn_fwd with its keys cut 14.0 against 8.1 us, uncut 8.5 / 4.4, gemm_bf16 7.2 / 3.9; calls of a decoding
-// step, host and GPU: attn_kv_fp8 21.4 / 11.2, kv_fp8_write 13.5 / 6.8, kv_fp8_read 15.8 / 7.2, rope_bf16 13.7 / 5.8.
+// step, host and GPU: attn_kv_fp8 21.4 / 9.9, kv_fp8_write 13.5 / 6.6, kv_fp8_read 15.8 / 7.2, rope_bf16 13.7 / 5.8.
 //
 // Each function returns None for everything that is not such a call, however slightly (another type, a subclass, a tensor of
 // a transform, a wrong shape), and the Python code then does what it always did, errors included; it returns an int for
