@@ -58,16 +58,22 @@ __device__ __forceinline__ unsigned largest(u32x4 w, unsigned m) {
 }
 
 // A unit is the keys or the values of one page and kv head, so that the page's exponent, its earlier tokens' codes and its new
-// ones are one unit's business: TPU = 64 threads for pages of up to 32 tokens, 256 for larger ones.  A thread reads blocks of 4
+// ones are one unit's business: a wavefront for pages of up to 32 tokens, 256 threads for larger ones.  A thread reads blocks of 4
 // tokens x 8 values, once, keeps them while the page's maximum is found, and packs the codes of V by four tokens: the transposed
-// page is put together in LDS and leaves in pieces of 16 tokens.  4 prompts of up to 4096 tokens, 8 heads of 128, pages of 64:
-// 16.2 us = 3.9 TB/s (37 us with a second pass over the values and single bytes of V); one token of 64 sequences, pages of 16 / 64
-// / 128: 7.1 / 9.5 / 12.4 us between two events (every column's byte of V lies in another line), 7.4 / 10.2 / 14.7 where scales grow.
-template <int D, int PAGE>
+// page is put together in LDS and leaves in pieces of 16 tokens; pieces with other tokens too were read before, and leave whole.
+// 4 prompts of up to 4096 tokens, 8 heads of 128, pages of 64: 16.1 us = 3.9 TB/s (37 us with a second pass over the values and
+// single bytes of V).
+// FEW: at most kFewTokens new tokens lie in few blocks and two pieces, for which a wavefront does on larger pages too: one token of
+// 99 sequences and 16 heads, pages of 64, 15.8 -> 11.3 us, 16 of 16 sequences and 8 heads, pages of 128, 8.4 -> 7.1 (17 tokens, by 256
+// threads, 8.6).  One token of 64 sequences, 8 heads, pages of 16 / 64 / 128: 5.3 / 6.9 / 7.4 us in a captured graph (every column's
+// byte of V lies in another line); 7.4 / 11.9 / 15.6 between two events where scales grow, 7.0 / 8.8 / 9.4 where they do not.
+constexpr int kFewTokens = 16;
+template <int D, int PAGE, bool FEW>
 __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
-    constexpr int TPU = PAGE <= 32 ? 64 : 256, UNITS = kThreads / TPU;
-    constexpr int CPR = D / 8, BLOCKS = PAGE / 4 * CPR, NB = (BLOCKS + TPU - 1) / TPU;
-    constexpr int PITCH = PAGE / 4 + 1;                                // dwords per row d of the page in LDS
+    constexpr int TPU = PAGE <= 32 || FEW ? 64 : 256, UNITS = kThreads / TPU;
+    constexpr int QS = FEW ? kFewTokens / 4 + 1 : PAGE / 4, CPR = D / 8, BLOCKS = QS * CPR, NB = (BLOCKS + TPU - 1) / TPU;
+    constexpr int PPR = FEW ? 2 : PAGE / 16, NP = D * PPR / TPU;       // pieces of 16 tokens of V per row d, and per thread
+    constexpr int PITCH = QS | 1;                                      // dwords per row d in LDS
     __shared__ unsigned s_page[UNITS][D * PITCH];
     __shared__ unsigned s_max[kThreads / 64];
     const int tid = threadIdx.x % TPU, sub = UNITS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / TPU);
@@ -94,14 +100,15 @@ __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
     const long long row = is_v ? p.v_ss : p.k_ss;
     const __bf16* const src = (is_v ? p.v + b * p.v_sb + h * p.v_sh : p.k + b * p.k_sb + h * p.k_sh) + (token0 - held) * row;   // of token 0 of the page
 
+    const int q0 = FEW ? held / 4 : 0, p0 = FEW ? held / 16 : 0;       // the first block and piece
     u32x4 x[NB][4];
     unsigned m = 0;
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-        const int blk = n * TPU + tid, q = blk / CPR, c = blk % CPR;
+        const int blk = n * TPU + tid, q = q0 + blk / CPR, c = blk % CPR;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int t = 4 * q + j;
+            const int t = blk < BLOCKS ? 4 * q + j : PAGE;
             x[n][j] = u32x4{0, 0, 0, 0};
             if (t >= held && t < held + fresh) x[n][j] = *(const u32x4*)(src + t * row + c * 8);
         }
@@ -112,6 +119,21 @@ __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
     unsigned char* const codes = (is_v ? p.c.v : p.c.k) + unit * PAGE * D;
     unsigned char* const exps = (is_v ? p.c.ve : p.c.ke) + unit;
     int e_old = fresh ? (int)*exps - 127 : 0;
+    // pieces of V that hold other tokens than new ones too
+    u32x4 old[NP];
+    auto piece_at = [&](int n, int& d) __attribute__((always_inline)) {
+        const int i = n * TPU + tid;
+        d = i / PPR;
+        return 16 * (p0 + i % PPR);
+    };
+    auto mixed = [&](int t) __attribute__((always_inline)) { return t < held + fresh && t + 16 > held && (t < held || t + 16 > held + fresh); };
+    if (is_v)
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+            int d;
+            const int t = piece_at(n, d);
+            if (fresh > 0 && mixed(t)) old[n] = *(const u32x4*)(codes + d * PAGE + t);
+        }
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -126,19 +148,20 @@ __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
     int e = exponent_for(__uint_as_float(m << 16));
     if (held > 0 && e < e_old) e = e_old;
 
-    // a scale that has grown: the earlier tokens' codes are rounded again, those of V where their pieces are written
+    // a scale that has grown: the earlier tokens' codes are rounded again, those of V that lie in a piece with new ones further down
     const bool grown = held > 0 && fresh > 0 && e > e_old;
     const float f2 = grown ? two_to(max(e_old - e, -126)) : 1.f;
-    if (grown && !is_v) {
-        for (int i = tid; i < held * (D / 16); i += TPU) {
-            u32x4* const c = (u32x4*)codes + i;
+    if (grown) {
+        const int first = held / 16, count = is_v ? D * first : held * (D / 16);
+        for (int i = tid; i < count; i += TPU) {
+            u32x4* const c = (u32x4*)(codes + (is_v ? i / first * PAGE + i % first * 16 : i * 16));
             *c = u32x4{again((*c)[0], f2), again((*c)[1], f2), again((*c)[2], f2), again((*c)[3], f2)};
         }
     }
     const float f1 = two_to(-e);
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-        const int blk = n * TPU + tid, q = blk / CPR, c = blk % CPR;
+        const int blk = n * TPU + tid, q = q0 + blk / CPR, c = blk % CPR;
         if (BLOCKS % TPU != 0 && blk >= BLOCKS) break;
         if (4 * q + 4 <= held || 4 * q >= held + fresh) continue;      // (no new token: what lies in LDS there is not used)
         u32x2 w[4];
@@ -154,38 +177,33 @@ __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int s = 8 * (i % 4);
-                s_page[sub][(c * 8 + i) * PITCH + q] = (w[0][i / 4] >> s & 0xff) | (w[1][i / 4] >> s & 0xff) << 8 | (w[2][i / 4] >> s & 0xff) << 16 | (w[3][i / 4] >> s & 0xff) << 24;
+                s_page[sub][(c * 8 + i) * PITCH + q - q0] = (w[0][i / 4] >> s & 0xff) | (w[1][i / 4] >> s & 0xff) << 8 | (w[2][i / 4] >> s & 0xff) << 16 | (w[3][i / 4] >> s & 0xff) << 24;
             }
         }
     }
-    if (is_v) {
+    if (is_v && fresh > 0) {
         if constexpr (TPU == 256) __syncthreads();
         else {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (a wavefront reads what it wrote itself)
             __builtin_amdgcn_wave_barrier();
         }
-        for (int i = tid; i < D * (PAGE / 16); i += TPU) {
-            const int d = i / (PAGE / 16), t = i % (PAGE / 16) * 16;
-            if (t >= held + fresh || (t + 16 <= held && !grown)) continue;
+#pragma unroll
+        for (int n = 0; n < NP; ++n) {
+            int d;
+            const int t = piece_at(n, d);
+            if (t >= held + fresh || t + 16 <= held) continue;
             u32x4 w;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = s_page[sub][d * PITCH + t / 4 + j];
-            u32x4* const piece = (u32x4*)(codes + d * PAGE + t);
-            if (grown && t < held) {                                   // earlier tokens, new ones, and what lies behind them
-                const u32x4 old = *piece;
+            for (int j = 0; j < 4; ++j) w[j] = s_page[sub][d * PITCH + min(max(t / 4 + j - q0, 0), QS - 1)];
+            if (mixed(t)) {                                            // earlier tokens, new ones, and what lies behind them
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     auto bytes = [](int n) __attribute__((always_inline)) { n = min(max(n, 0), 4); return n == 4 ? ~0u : (1u << (8 * n)) - 1; };
                     const unsigned was = bytes(held - t - 4 * j), now = bytes(held + fresh - t - 4 * j) & ~was;
-                    w[j] = (again(old[j], f2) & was) | (w[j] & now) | (old[j] & ~(was | now));
+                    w[j] = ((grown ? again(old[n][j], f2) : old[n][j]) & was) | (w[j] & now) | (old[n][j] & ~(was | now));
                 }
-                *piece = w;
-            } else if (t >= held && t + 16 <= held + fresh) *piece = w;
-            else {
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (t + j >= held && t + j < held + fresh) codes[d * PAGE + t + j] = (unsigned char)(w[j / 4] >> (8 * (j % 4)));
             }
+            *(u32x4*)(codes + d * PAGE + t) = w;
         }
     }
     if (tid == 0 && fresh > 0) *exps = (unsigned char)(e + 127);
@@ -299,22 +317,25 @@ __global__ __launch_bounds__(kThreads) void kv_read(KvReadParams p) {
 
 }  // namespace
 
-template <int PAGE>
+template <int PAGE, bool FEW>
 static void launch_write(const KvWriteParams& p, dim3 grid, hipStream_t stream) {
-    if (p.c.D == 128) hipLaunchKernelGGL((kv_write<128, PAGE>), grid, dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL((kv_write<64, PAGE>), grid, dim3(kThreads), 0, stream, p);
+    if (p.c.D == 128) hipLaunchKernelGGL((kv_write<128, PAGE, FEW>), grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL((kv_write<64, PAGE, FEW>), grid, dim3(kThreads), 0, stream, p);
 }
 
 int kv_write_launch(const KvWriteParams& p, hipStream_t stream) {
     const double units = (double)p.B * p.F * p.c.Hkv;
-    const int per = p.c.page <= 32 ? 4 : 1;
+    const bool few = p.c.page >= 64 && p.S <= kFewTokens;
+    const int per = p.c.page <= 32 || few ? 4 : 1;
     const double blocks = (units + per - 1) / per;
     if (blocks * kThreads >= 4294967296.0) return -2;
     const dim3 grid((unsigned)blocks, 2);
-    if (p.c.page == 16) launch_write<16>(p, grid, stream);
-    else if (p.c.page == 32) launch_write<32>(p, grid, stream);
-    else if (p.c.page == 64) launch_write<64>(p, grid, stream);
-    else launch_write<128>(p, grid, stream);
+    if (p.c.page == 16) launch_write<16, false>(p, grid, stream);
+    else if (p.c.page == 32) launch_write<32, false>(p, grid, stream);
+    else if (p.c.page == 64 && few) launch_write<64, true>(p, grid, stream);
+    else if (p.c.page == 64) launch_write<64, false>(p, grid, stream);
+    else if (few) launch_write<128, true>(p, grid, stream);
+    else launch_write<128, false>(p, grid, stream);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 

@@ -3,7 +3,7 @@
 // A thread owns V pairs of columns of one token (or columns that are only copied) and walks heads, those of q and k as one
 // range: the angle is the same for all of them, so its sine and cosine are made once, in registers, and no table is read.
 // What bounds it: reading and writing every value once.  40 heads of 16384 tokens, all 128 columns turned (336 MB in and out),
-// 65.6 us = 5.1 TB/s, where a copy of torch reaches 4.9; 32 heads of 8192 tokens, half the columns turned, 29.5 us = 4.5 TB/s;
+// 65.6 us = 5.1 TB/s, where a copy of torch reaches 4.9; 32 heads of 8192 tokens, half the columns turned, 27 us = 5.0 TB/s;
 // 40 heads of 64 tokens 3.1 us in a captured graph: latency.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -22,8 +22,10 @@ constexpr int kThreads = 256;
 // every CU: with 40 heads of 16384 tokens 8 / 20 / 4 / 1 heads take 69 / 79 / 78 / 90 us, with 48 heads of 4096 tokens
 // 6 / 2 / 1 parts of the heads (1152 / 384 / 192 workgroups) 26 / 42 / 61 us.
 constexpr int kHeads = 8, kLeastBlocks = 768;
-// Results are not read again here: stored past the caches (48 heads of 4096 tokens 25.9 -> 19.2 us, 40 of 16384 69 -> 67).
-// Values are loaded past them too where there are more than the memory-side cache keeps until they could be used again (72
+// Results are not read again here.  Rows that one instruction stores whole (neighbours) go past the caches, 40 heads of 16384
+// tokens 67.6 -> 65.9 us; halves are put together in L2: stored past it, 32 heads of 27720 tokens, 16 of 64 columns turned, take
+// 113 us in place of 62 (and 145 where turned and copied columns are not stored side by side in one loop).
+// Values are loaded past the caches where there are more than the memory-side cache keeps until they could be used again (72
 // heads of 30000 tokens 199 -> 192 us, but 48 of 4096, which repeated calls find there, 19 -> 25).
 constexpr double kStreamed = 128e6;
 
@@ -39,21 +41,27 @@ __device__ __forceinline__ typename Chunk<N>::type fetch(const __bf16* p) {
     if constexpr (ST) return __builtin_nontemporal_load(from);
     else return *from;
 }
-template <int N, bool ST>
-__device__ __forceinline__ void load(const __bf16* p, float (&x)[N]) {
+template <int N>
+__device__ __forceinline__ void values(typename Chunk<N>::type raw, float (&x)[N]) {
     typedef __attribute__((ext_vector_type(N))) unsigned short bits_t;
-    const bits_t b = __builtin_bit_cast(bits_t, fetch<N, ST>(p));
+    const bits_t b = __builtin_bit_cast(bits_t, raw);
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = __uint_as_float((unsigned)b[i] << 16);
 }
 template <int N>
-__device__ __forceinline__ void store(__bf16* p, const float (&x)[N]) {
+__device__ __forceinline__ typename Chunk<N>::type rounded(const float (&x)[N]) {
     typedef __attribute__((ext_vector_type(N))) float f_t;
     typedef __attribute__((ext_vector_type(N))) __bf16 b_t;
     f_t f;
 #pragma unroll
     for (int i = 0; i < N; ++i) f[i] = x[i];
-    __builtin_nontemporal_store(__builtin_bit_cast(typename Chunk<N>::type, __builtin_convertvector(f, b_t)), (typename Chunk<N>::type*)p);
+    return __builtin_bit_cast(typename Chunk<N>::type, __builtin_convertvector(f, b_t));
+}
+template <int N, bool PAST>
+__device__ __forceinline__ void store(__bf16* p, typename Chunk<N>::type raw) {
+    auto* const to = (typename Chunk<N>::type*)p;
+    if constexpr (PAST) __builtin_nontemporal_store(raw, to);
+    else *to = raw;
 }
 
 // x0 a + x1 b, in one order of roundings wherever it stands: a result does not depend on the other heads and tokens of a call.
@@ -80,47 +88,47 @@ __global__ __launch_bounds__(kThreads) void rope_turn(RopeParams p) {
         }
     };
 
+    // turned columns: pairs f ... f + V - 1; behind them copies.  Both in one stream, so that rows are read and written whole.
+    constexpr int W = IL ? 2 * V : V;
     const int f = item * V;
-    if (f >= p.R / 2) {                                 // behind the turned columns: copies
-        constexpr int W = IL ? 2 * V : V;
-        const int col = p.R + (item - p.R / 2 / V) * W;
-        heads([&](const __bf16* in, __bf16* out) __attribute__((always_inline)) {
-            __builtin_nontemporal_store(fetch<W, ST>(in + col), (typename Chunk<W>::type*)(out + col));
-        });
-        return;
-    }
-    float c[V], sn[V];
-    const double pos = (double)p.positions[b * p.pos_pitch + s];
+    const bool turns = f < p.R / 2;
+    const int col = turns ? (IL ? 2 * f : f) : p.R + (item - p.R / 2 / V) * W, other = p.R / 2 + f;
+    float c[V] = {}, sn[V] = {};
+    if (turns) {
+        const double pos = (double)p.positions[b * p.pos_pitch + s];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const double turns = pos * (p.inv_freq[f + i] * 0.15915494309189533577);
-        const float part = (float)(turns - rint(turns));       // of a turn, in [-1/2, 1/2]
-        sincospif(2.f * part, &sn[i], &c[i]);
-        c[i] *= p.mscale;
-        sn[i] *= p.mscale * p.sign;
+        for (int i = 0; i < V; ++i) {
+            const double angle = pos * (p.inv_freq[f + i] * 0.15915494309189533577);      // in turns
+            const float part = (float)(angle - rint(angle));       // of a turn, in [-1/2, 1/2]
+            sincospif(2.f * part, &sn[i], &c[i]);
+            c[i] *= p.mscale;
+            sn[i] *= p.mscale * p.sign;
+        }
     }
     heads([&](const __bf16* in, __bf16* out) __attribute__((always_inline)) {
+        typename Chunk<W>::type first = fetch<W, ST>(in + col);
         if constexpr (IL) {
-            float x[2 * V], y[2 * V];
-            load<2 * V, ST>(in + 2 * f, x);
+            float x[W], y[W];
+            values<W>(first, x);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 y[2 * i] = turned(x[2 * i], c[i], -x[2 * i + 1], sn[i]);
                 y[2 * i + 1] = turned(x[2 * i], sn[i], x[2 * i + 1], c[i]);
             }
-            store<2 * V>(out + 2 * f, y);
-        } else {
+            if (turns) first = rounded<W>(y);
+        } else if (turns) {
             float x0[V], x1[V], y0[V], y1[V];
-            load<V, ST>(in + f, x0);
-            load<V, ST>(in + p.R / 2 + f, x1);
+            values<V>(first, x0);
+            values<V>(fetch<V, ST>(in + other), x1);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 y0[i] = turned(x0[i], c[i], -x1[i], sn[i]);
                 y1[i] = turned(x0[i], sn[i], x1[i], c[i]);
             }
-            store<V>(out + f, y0);
-            store<V>(out + p.R / 2 + f, y1);
+            first = rounded<V>(y0);
+            store<V, IL>(out + other, rounded<V>(y1));
         }
+        store<W, IL>(out + col, first);
     });
 }
 

@@ -180,3 +180,16 @@ def test_strided_rows_and_a_part_of_a_wider_table():
                 assert np.array_equal(out[:m], ref[3:3 + m]) and not out[m:].any()
     ko.fill_(7.0), vo.fill_(7.0)
     assert (room == 7.0).all()
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("S", [1, 16, 17, 90])
+def test_a_start_inside_a_missing_page(page, S):
+    """The first new tokens would lie behind others of a page that is not there; every start in a page, few tokens and more."""
+    rng = np.random.default_rng(page + S)
+    D, starts = 64, [page + 5, 7, 2 * page - 1, page - 4, 3]
+    table, P = make_table(rng, [s + S for s in starts], page)
+    table[0, 1], table[1, 0], table[2, 1] = -1, P, 2 ** 31 - 1
+    cache = make_cache(rng, P, 2, page, D)
+    k, v = (bf16(rng.standard_normal((len(starts), 2, S, D)) * 2.0 ** rng.integers(-6, 7, (len(starts), 2, S, 1))) for _ in range(2))
+    check(*run_write(cache, table, k, v, starts, None))
