@@ -221,6 +221,7 @@ __device__ __forceinline__ void decode16(u32x4 c, float scale, unsigned (&out)[8
 // 64 positions of one sequence and kv head, keys (blockIdx.y 0) or values.  Keys go straight through; a thread with values holds
 // 16 tokens of two columns, which meet their rows in LDS (dword c of the rows of group g lies at c ^ 16 g: no bank conflicts).
 // 8 sequences of up to 4001 positions, 8 heads of 128: 34.5 us a call = 4.9 TB/s (25 in the kernel while the codes are still cached).
+// A few positions of many sequences cost a line of V for every column: three of 12540 sequences, 4 heads, pages of 64, 140 us.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv_read(KvReadParams p) {
     constexpr int CPR = D / 16, NK = kReadRows * CPR / kThreads;
