@@ -806,22 +806,22 @@ __global__ __launch_bounds__(256) void attn_kv_join(KvAttnParams p) {
 
 }  // namespace
 
-// Time of a call in microseconds, from what was measured on shapes of 1 to 128 sequences, 300 to 64000 keys, 1 to 256 packed rows.
+// Time of a call in microseconds, from what was measured on shapes of 1 to 256 sequences, 1 to 64000 keys, 1 to 256 packed rows.
 // A round of workgroups takes its start (lengths, page numbers, first codes) and end, and for its tiles the longer of what their
 // arithmetic takes, which two workgroups of four wavefronts on a CU share, and of what HBM takes at 6.2 TB/s, or up to 1.4
 // times that where both are alike.  Parts cost a second kernel and their traffic.
 static double estimate(const KvAttnPlan& plan, long long pairs, long long rows, int tiles, int D) {
-    const bool rows16 = plan.rows == kBlock, wide = D == 128;
-    const long long n = pairs * plan.row_wgs * plan.splits, slots = rows16 && plan.waves == 8 ? 256 : wide ? 512 : 768;
-    const double start = rows16 ? (plan.waves == 8 ? (wide ? 6.6 : 5.6) : wide ? 5.2 : 4.8) : 6.5;
-    // a step is a tile of every wavefront (rows) or of the workgroup: with one workgroup on a CU, with two, and with the CU full
-    const double alone = rows16 ? (plan.waves == 8 ? (wide ? 2.5 : 1.0) : wide ? 1.3 : 0.72) : wide ? 1.21 : 0.95;
-    const double full = rows16 ? (plan.waves == 8 ? alone : wide ? 2.1 : 1.6) : wide ? 2.07 : 1.87;
+    const bool rows16 = plan.rows == kBlock, wide = D == 128, single = plan.waves == 1;
+    const long long n = pairs * plan.row_wgs * plan.splits, slots = rows16 && plan.waves == 8 ? 256 : (wide ? 2048 : 3072) / plan.waves;
+    const double start = single ? 4.6 : rows16 ? (plan.waves == 8 ? (wide ? 6.6 : 5.6) : wide ? 5.2 : 4.8) : 6.5;
+    // a step is a tile of every wavefront (rows) or of the workgroup: with one wavefront on a SIMD, with two, and with the CU full
+    const double alone = single ? (wide ? 0.95 : 0.6) : rows16 ? (plan.waves == 8 ? (wide ? 2.5 : 1.0) : wide ? 1.3 : 0.72) : wide ? 1.21 : 0.95;
+    const double full = single ? (wide ? 1.6 : 1.2) : rows16 ? (plan.waves == 8 ? alone : wide ? 2.1 : 1.6) : wide ? 2.07 : 1.87;
     const double two = rows16 || wide ? full : 1.33;
     const int per = (tiles + plan.splits - 1) / plan.splits, steps = rows16 ? (per + plan.waves - 1) / plan.waves : per;
     const double bytes = (double)tiles / plan.splits * kTile * D * 2 / plan.row_wgs;          // of a workgroup, its row blocks sharing an L2
     auto round = [&](long long wgs) {
-        const double work = steps * (wgs <= 256 ? alone : wgs <= 512 ? two : full), hbm = wgs * bytes / 6.2e6;
+        const double work = steps * (wgs * plan.waves <= 1024 ? alone : wgs * plan.waves <= 2048 ? two : full), hbm = wgs * bytes / 6.2e6;
         const double both = sqrt(work * work + hbm * hbm) * (rows16 && plan.waves == 8 ? 0.9 : 1.0);
         return start + (both > work ? (both > hbm ? both : hbm) : work);
     };
@@ -836,24 +836,28 @@ static double estimate(const KvAttnPlan& plan, long long pairs, long long rows, 
 
 // How many rows a workgroup takes, by how many wavefronts, and how the keys are cut: whatever is estimated to be the fastest.
 // Measured, rows of 16 / of 128 per workgroup, sequences x keys, D = 128, 8 kv heads: 32 packed rows 1 x 64000 35.5 / 47.0 us,
-// 64 x 1000 39.5 / 45.0; 64 rows 55.9 / 50.2, 61.1 / 46.6; 128 rows 96.6 / 57.4, but 1 x 1000 11.6 / 16.2.
+// 64 x 1000 39.5 / 45.0; 64 rows 55.9 / 50.2, 61.1 / 46.6; 128 rows 96.6 / 57.4, but 1 x 1000 11.6 / 16.2.  A wavefront by itself
+// or four, sequences x keys, 8 kv heads of 128: 256 x 60 11.1 / 22.4 us, 256 x 250 30.2 / 36.5, but 16 x 250 8.4 / 6.4; where several
+// row blocks share keys that are cut it is slower than estimated (2 blocks, 1 x 3781 14.0 / 11.2), and left out.
 KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits, int wg_rows) {
     static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
     const long long R = (long long)(Hq / Hkv) * Sq, pairs = (long long)B * Hkv, rows = (long long)B * Hq * Sq;
     const int tiles = (keys + kTile - 1) / kTile;
     KvAttnPlan best{};
     double least = 1e300;
-    for (int kind = 0; kind < 3; ++kind) {
+    static const int kWaves[] = {8, 4, 1, kTileWaves};
+    for (int kind = 0; kind < 4; ++kind) {
         KvAttnPlan plan;
-        plan.rows = kind < 2 ? kBlock : kTileWaves * kTileRows;
-        if (wg_rows ? plan.rows != wg_rows : kind < 2 && R > 512) continue;
-        plan.waves = kind == 0 ? 8 : 4;
+        plan.rows = kind < 3 ? kBlock : kTileWaves * kTileRows;
+        if (wg_rows ? plan.rows != wg_rows : kind < 3 && R > 512) continue;
+        plan.waves = kWaves[kind];
         plan.row_wgs = (int)((R + plan.rows - 1) / plan.rows);
         plan.keys = keys;
-        const int most = kind < 2 ? (tiles + plan.waves - 1) / plan.waves : (tiles + 1) / 2;
+        const int most = kind < 3 ? (tiles + plan.waves - 1) / plan.waves : (tiles + 1) / 2;
         for (int cut : kCuts) {
             if (splits == 0 && cut > 1 && cut > most) break;
             plan.splits = splits ? splits : cut;
+            if (plan.waves == 1 && plan.splits > 1 && plan.row_wgs > 1) break;
             // (a given cut that is the library's own gets the shape that the library chose for it)
             const double t = estimate(plan, pairs, rows, tiles, D) + (plan.splits > 1 && plan.splits > most ? 1e9 : 0.0);
             if (t < least) { least = t; best = plan; }
@@ -866,6 +870,7 @@ KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int spl
 template <int D>
 static void launch(const KvAttnParams& p, const KvAttnPlan& plan, unsigned blocks, hipStream_t stream) {
     if (plan.rows == kBlock && plan.waves == 8) hipLaunchKernelGGL((attn_kv_rows<D, 8>), dim3(blocks), dim3(512), 0, stream, p);
+    else if (plan.waves == 1) hipLaunchKernelGGL((attn_kv_rows<D, 1>), dim3(blocks), dim3(64), 0, stream, p);
     else if (plan.rows == kBlock) hipLaunchKernelGGL((attn_kv_rows<D, 4>), dim3(blocks), dim3(256), 0, stream, p);
     else hipLaunchKernelGGL(attn_kv_tiles<D>, dim3(blocks), dim3(kTileWaves * 64), 0, stream, p);
 }

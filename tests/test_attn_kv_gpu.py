@@ -327,3 +327,18 @@ def test_two_calls_at_once():
     for i in range(2):
         for o, lse in got[i]:
             assert torch.equal(o, want[i][0]) and torch.equal(lse, want[i][1])
+
+
+@pytest.mark.parametrize("D,window,Sq", [(64, 0, 1), (128, 0, 1), (64, 30, 2), (128, 9, 5)])
+def test_many_short_sequences(D, window, Sq):
+    """Where a wavefront by itself takes a sequence's head: 0 to 130 keys, some pages missing, NaN behind the ends."""
+    rng = np.random.default_rng(D + window)
+    lens = [int(n) for n in rng.integers(0, 131, 200)]
+    table, P = make_table(rng, lens, 16)
+    table[rng.random(table.shape) < 0.05] = -1
+    cache = make_cache(rng, P, 2, 16, D)
+    spoil_behind(cache, table, lens)
+    q = bf16(rng.standard_normal((200, 6, Sq, D)))
+    want = attn_reference(q, cache, table, lens, None, True, window, 2 if window else 0, D ** -0.5)
+    for limit in (0, 131):
+        check(run(q, cache, table, lens, window=window, sinks=2 if window else 0, max_len=limit), want)
