@@ -342,3 +342,17 @@ def test_many_short_sequences(D, window, Sq):
     want = attn_reference(q, cache, table, lens, None, True, window, 2 if window else 0, D ** -0.5)
     for limit in (0, 131):
         check(run(q, cache, table, lens, window=window, sinks=2 if window else 0, max_len=limit), want)
+
+
+@pytest.mark.parametrize("D,window,Sq", [(64, 0, 1), (128, 0, 1), (128, 70, 2)])
+def test_a_batch_with_a_few_long_sequences(D, window, Sq):
+    """Where eight wavefronts share a sequence's head: 32 sequences, some with 1500 keys, most with few, some with none."""
+    rng = np.random.default_rng(D + Sq)
+    lens = [1500, 1337, 1024] + [int(n) for n in rng.integers(0, 160, 29)]
+    table, P = make_table(rng, lens, 16)
+    table[0, 3], table[1, 80] = -1, P
+    cache = make_cache(rng, P, 8, 16, D)
+    spoil_behind(cache, table, lens)
+    q = bf16(rng.standard_normal((32, 16, Sq, D)))
+    want = attn_reference(q, cache, table, lens, None, True, window, 3 if window else 0, D ** -0.5)
+    check(run(q, cache, table, lens, window=window, sinks=3 if window else 0), want)
