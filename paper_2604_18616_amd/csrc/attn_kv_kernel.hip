@@ -15,7 +15,7 @@
 // the workgroups of a row by attn_kv_join or attn_kv_combine from fp32 parts.
 // What bounds it: reading the codes, or latency.  32 sequences of up to 8191 keys, 8 kv heads of 128: 63 us = 4.4 TB/s; 16 of up to
 // 20000 keys with a window of 4096, 16 heads of 64: 25 us = 5.0 TB/s (a copy reaches 4.9); one of 131071 keys, one kv head: 13.6 us
-// (11 and 4 in the two kernels); one of 2000 keys, 8 kv heads: 10 us (7 and 3.5).  Many rows have a kernel of their own below.
+// (10 and 3.5 in the two kernels); one of 2000 keys, 8 kv heads: 10 us (6 and 4).  Many rows have a kernel of their own below.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <math.h>

@@ -61,7 +61,7 @@ __device__ __forceinline__ unsigned largest(u32x4 w, unsigned m) {
 // ones are one unit's business: a wavefront for pages of up to 32 tokens, 256 threads for larger ones.  A thread reads blocks of 4
 // tokens x 8 values, once, keeps them while the page's maximum is found, and packs the codes of V by four tokens: the transposed
 // page is put together in LDS and leaves in pieces of 16 tokens; pieces with other tokens too were read before, and leave whole.
-// 4 prompts of up to 4096 tokens, 8 heads of 128, pages of 64: 16.1 us = 3.9 TB/s (37 us with a second pass over the values and
+// 4 prompts of up to 4096 tokens, 8 heads of 128, pages of 64: 14.8 us = 4.2 TB/s (37 us with a second pass over the values and
 // single bytes of V).
 // FEW: at most kFewTokens new tokens lie in few blocks and two pieces, for which a wavefront does on larger pages too: one token of
 // 99 sequences and 16 heads, pages of 64, 15.8 -> 11.3 us, 16 of 16 sequences and 8 heads, pages of 128, 8.4 -> 7.1 (17 tokens, by 256
