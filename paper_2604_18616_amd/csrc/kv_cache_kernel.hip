@@ -1,6 +1,7 @@
 // Writing the quantised cache and reading it back, for gfx950.  What bounds both: reading and writing every value once, or, for
 // a token per sequence, a chain of latencies (lengths, page, exponent).
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "gfx950_prims.h"
@@ -221,7 +222,6 @@ __device__ __forceinline__ void decode16(u32x4 c, float scale, unsigned (&out)[8
 // 64 positions of one sequence and kv head, keys (blockIdx.y 0) or values.  Keys go straight through; a thread with values holds
 // 16 tokens of two columns, which meet their rows in LDS (dword c of the rows of group g lies at c ^ 16 g: no bank conflicts).
 // 8 sequences of up to 4001 positions, 8 heads of 128: 34.5 us a call = 4.9 TB/s (25 in the kernel while the codes are still cached).
-// A few positions of many sequences cost a line of V for every column: three of 12540 sequences, 4 heads, pages of 64, 140 us.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv_read(KvReadParams p) {
     constexpr int CPR = D / 16, NK = kReadRows * CPR / kThreads;
@@ -316,6 +316,80 @@ __global__ __launch_bounds__(kThreads) void kv_read(KvReadParams p) {
     }
 }
 
+// The same for at most kFewTokens positions, which lie in two groups of 16: keys (blockIdx.y 0) by pieces of 16 columns of rows one
+// after the other, values by a wavefront per sequence and head whose lanes take two columns each.  Heads x sequences of 128 columns:
+// one position of 8 x 6767, pages of 16, 121 -> 33 us; 8 of 8 x 3296 73 -> 34; 16 of 8 x 1000 23.1 -> 20.5 (17: 24); 16 of 8 x 16 3.3 and
+// 3.7.  What a few positions cannot do without is a piece of a line of V for every column: three of 4 x 12540, pages of 64, 108 us.
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv_read_few(KvReadParams p) {
+    constexpr int CPR = D / 16, UNITS = kThreads / 64;
+    __shared__ __attribute__((aligned(16))) unsigned s_rows[UNITS][kFewTokens * D / 2];
+    const int page = p.c.page;
+    auto lookup = [&](int b, int n, long long pos) __attribute__((always_inline)) {
+        if (pos >= n || (pos >> p.c.page_log2) >= p.c.W) return -1;
+        const int at = p.c.table[b * p.c.pitch + (pos >> p.c.page_log2)];
+        return at >= 0 && at < p.c.P ? at : -1;
+    };
+    if (blockIdx.y == 0) {
+        const unsigned id = blockIdx.x * kThreads + threadIdx.x, row = id / CPR, bh = row / (unsigned)p.S;
+        const int c = id % CPR, s = row - bh * p.S, b = bh / (unsigned)p.c.Hkv, h = bh - b * p.c.Hkv;
+        if (b >= p.B) return;
+        const long long pos = (long long)p.first + s;
+        const int at = lookup(b, p.lens[b], pos);
+        u32x4 codes = {0, 0, 0, 0};
+        float scale = 1.f;
+        if (at >= 0) {
+            const size_t unit = (size_t)at * p.c.Hkv + h;
+            codes = *(const u32x4*)(p.c.k + (unit * page + (pos & (page - 1))) * D + 16 * c);
+            scale = __uint_as_float((unsigned)p.c.ke[unit] << 23);
+        }
+        unsigned w[8];
+        decode16(codes, scale, w);
+        u32x4* const o = (u32x4*)(p.k + b * p.k_sb + h * p.k_sh + s * p.k_ss + 16 * c);
+        o[0] = u32x4{w[0], w[1], w[2], w[3]};
+        o[1] = u32x4{w[4], w[5], w[6], w[7]};
+        return;
+    }
+    const int lane = threadIdx.x & 63, sub = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned id = blockIdx.x * UNITS + sub;
+    const int b = (int)(id / (unsigned)p.c.Hkv), h = (int)(id % (unsigned)p.c.Hkv);
+    if (b >= p.B) return;                                              // (no barrier below: a wavefront reads what it wrote itself)
+    const int n = p.lens[b], skip = p.first & 15, d = 2 * lane;
+    if (d < D)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            if (16 * g - skip >= p.S) break;
+            const long long pos = (long long)p.first - skip + 16 * g;
+            // (a group that begins before the first position is there if that position is)
+            const int at = lookup(b, n, g == 0 ? (long long)p.first : pos);
+            u32x4 c[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+            float scale = 1.f;
+            if (at >= 0) {
+                const size_t unit = (size_t)at * p.c.Hkv + h;
+                const unsigned char* const v = p.c.v + unit * page * D + d * page + (pos & (page - 1));
+                c[0] = *(const u32x4*)v;
+                c[1] = *(const u32x4*)(v + page);
+                scale = __uint_as_float((unsigned)p.c.ve[unit] << 23);
+            }
+            unsigned w0[8], w1[8];
+            decode16(c[0], scale, w0);
+            decode16(c[1], scale, w1);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int t = 16 * g + j - skip;
+                const unsigned x = 16 * (j % 2), pair = (w0[j / 2] >> x & 0xffff) | (w1[j / 2] >> x) << 16;
+                if (t >= 0 && t < p.S) s_rows[sub][t * (D / 2) + lane] = pos + j < n ? pair : 0u;
+            }
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    __bf16* const out = p.v + b * p.v_sb + h * p.v_sh;
+    for (int i = lane; i < p.S * (D / 8); i += 64) {
+        const int t = i / (D / 8), c = i % (D / 8);
+        *(u32x4*)(out + t * p.v_ss + 8 * c) = *(const u32x4*)&s_rows[sub][t * (D / 2) + 4 * c];
+    }
+}
+
 }  // namespace
 
 template <int PAGE, bool FEW>
@@ -341,10 +415,14 @@ int kv_write_launch(const KvWriteParams& p, hipStream_t stream) {
 }
 
 int kv_read_launch(const KvReadParams& p, hipStream_t stream) {
-    const double blocks = (double)p.B * p.c.Hkv * ((p.S + kReadRows - 1) / kReadRows);
+    const bool few = p.S <= kFewTokens;
+    const double units = (double)p.B * p.c.Hkv;
+    const double blocks = few ? fmax(ceil(units * p.S * (p.c.D / 16) / kThreads), ceil(units / (kThreads / 64))) : units * ((p.S + kReadRows - 1) / kReadRows);
     if (blocks * kThreads >= 4294967296.0) return -2;
     const dim3 grid((unsigned)blocks, 2);
-    if (p.c.D == 128) hipLaunchKernelGGL(kv_read<128>, grid, dim3(kThreads), 0, stream, p);
+    if (few && p.c.D == 128) hipLaunchKernelGGL(kv_read_few<128>, grid, dim3(kThreads), 0, stream, p);
+    else if (few) hipLaunchKernelGGL(kv_read_few<64>, grid, dim3(kThreads), 0, stream, p);
+    else if (p.c.D == 128) hipLaunchKernelGGL(kv_read<128>, grid, dim3(kThreads), 0, stream, p);
     else hipLaunchKernelGGL(kv_read<64>, grid, dim3(kThreads), 0, stream, p);
     return hipGetLastError() == hipSuccess ? 0 : -1;
 }

@@ -193,3 +193,30 @@ def test_a_start_inside_a_missing_page(page, S):
     cache = make_cache(rng, P, 2, page, D)
     k, v = (bf16(rng.standard_normal((len(starts), 2, S, D)) * 2.0 ** rng.integers(-6, 7, (len(starts), 2, S, 1))) for _ in range(2))
     check(*run_write(cache, table, k, v, starts, None))
+
+
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 16), (128, 128), (64, 64)])
+@pytest.mark.parametrize("S,first", [(1, 0), (1, 31), (3, 15), (16, 0), (16, 1), (16, 47), (7, 64), (17, 15), (5, 2 ** 31 - 1)])
+def test_reading_a_few_positions(D, page, S, first):
+    """Up to 16 positions, which may lie in two pages of which one is missing, before, across and behind a sequence's end."""
+    import torch
+    from paper_2604_18616_amd import binding
+    rng = np.random.default_rng(S + page)
+    lens = [0, 1, 16, 33, 50, 64, 200]
+    table, P = make_table(rng, lens, page)
+    if table.shape[1] > 2:
+        table[3, 1], table[5, 2], table[6, 3] = -1, P, -7
+    cache = make_cache(rng, P, 3, page, D, spread=20)
+    dev, tab = to_cuda(cache, table)
+    room = torch.full((len(lens), S, 6, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    k, v = (room[:, :, h:h + 3].transpose(1, 2) for h in (0, 3))
+    binding.kv_fp8_read(dev, tab, whole(lens), S, first=first, k=k, v=v)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lens):
+        for h in range(3):
+            wk, wv, _ = gather_reference(cache, table, b, h, n)
+            for got, ref in ((host(k)[b, h], wk), (host(v)[b, h], wv)):
+                want = np.zeros((S, D))
+                m = max(0, min(S, n - first))
+                want[:m] = ref[first:first + m]
+                assert np.array_equal(got, want), (b, h)
