@@ -245,15 +245,18 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
     };
     auto weigh = [&](int t) __attribute__((always_inline)) {
         const int key0 = tile_of(t) * kTile;
-        const float scale = __uint_as_float(ve << 23);
+        float scale = __uint_as_float(ve << 23);
         if (at_edge(key0, at_v)) {
-            // NaN codes become zero: the probability 0 of a row that does not see them must not meet them
-            const unsigned some = sees(key0 + 16 * grp, hi_all, lo_all, at_v >= 0);
+            // Keys without a page have zeros: what was loaded for them are page 0's codes and exponent, which may stand for anything.
+            // NaN codes become zero: the probability 0 of a row that does not see them must not meet them.
+            const unsigned some = sees(key0 + 16 * grp, hi_all, lo_all, at_v >= 0), there = at_v >= 0 ? ~0u : 0u;
+            scale = at_v >= 0 ? scale : 1.f;
             unsigned bad = 0;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
+                    vr[d][j] &= there;
                     const unsigned nan = nan_codes(vr[d][j]) >> 7;
                     vr[d][j] &= ~(nan * 0xffu);
                     bad |= (nan * 0x10204080u >> 28) << (4 * j);                      // bytes 0 ... 3 to bits 0 ... 3
@@ -480,7 +483,8 @@ __global__ __launch_bounds__(kTileWaves * 64, D == 64 ? 3 : 2) void attn_kv_tile
         ve = *(ScalarWords)(va & ~3ull);
         shifts = (unsigned)(ea & 3) | (unsigned)(va & 3) << 8;
     };
-    // What tile t, loaded, needs before it is decoded: zeros where the sequence holds nothing, a note of groups without a page.
+    // What tile t, loaded, needs before it is decoded: zeros where the sequence holds nothing, a note of groups without a page (for
+    // which page 0 was loaded: its exponents, which may be any byte, do not count).
     // At an edge NaN must not meet the probability 0 of a row that does not see it: zeros too, and a note.
     auto mend = [&](int t) __attribute__((always_inline)) {
         if (t < whole && !gap) return;
@@ -502,7 +506,10 @@ __global__ __launch_bounds__(kTileWaves * 64, D == 64 ? 3 : 2) void attn_kv_tile
                 if (bits) s_nan[t & 1] = t;
             }
         }
-        if (gap) s_gone[t & 1][wave] = t;
+        if (gap) {
+            s_gone[t & 1][wave] = t;
+            ke = ve = 0x7f7f7f7f;
+        }
     };
     // Lane offsets into a stage; the pieces of a row are found by exchanging address bits.
     unsigned k_read = piece_offset<KP>(key_of_row(lane & 31), half), v_read = kTile * D * 2 + piece_offset<8>(lane & 31, half);
