@@ -79,7 +79,9 @@ int kv_fp8_read(const KvFp8Cache *cache, const int *table, long long table_pitch
  *     q, o  bf16 [B, Hq, Sq, D]  (strided)     lse  fp32 [B, Hq, Sq] contiguous, may be NULL      lens, q_lens  int32 [B]
  * Scores, the running maximum and sum and the output are fp32; the probabilities are rounded to bf16 as the second operand
  * of the matrix instruction, o once when it is stored.  A row that sees no key, and rows i >= q_lens[b], get o = 0 and
- * lse = -inf.  A NaN in the cache reaches the rows that see it and no others, whatever lies behind the mask.
+ * lse = -inf.  NaN and infinities (codes of 256 and more at the exponent 120) in the cache reach the rows that see them and no
+ * others, whatever lies behind the mask, behind the last token, or on pages that no sequence holds, codes and exponents.  An infinity
+ * in the values makes its column of those rows infinite, or NaN where it meets the other sign or its probability is 0 in fp32.
  * max_len: no sequence is longer, which the library counts on when it divides the work (0: width * page); lens is taken
  * as at most max_len (and as at most width * page), q_lens as 0 ... Sq.  lens may be less than q_lens: the rows at negative
  * positions see no key under a causal mask.

@@ -83,6 +83,14 @@ __device__ __forceinline__ bf16x8 decode(unsigned lo, unsigned hi, float scale) 
 }
 // The bytes of w that are the NaN code, as 0x80 each.
 __device__ __forceinline__ unsigned nan_codes(unsigned w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// Those that do not stand for a number in bf16, given the biased exponent: with the largest one that is written, 2^120, codes from
+// 0x78 on, which are 256 and more, are infinities too.
+__device__ __forceinline__ unsigned no_numbers(unsigned w, unsigned exponent) {
+    return ((w & 0x7f7f7f7fu) + (exponent == 247 ? 0x08080808u : 0x01010101u)) & 0x80808080u;
+}
+// Of these, those that make a sum infinite upwards (without their sign) or downwards; NaN does both.
+__device__ __forceinline__ unsigned upwards(unsigned w, unsigned odd) { return odd & (~w | nan_codes(w)); }
+__device__ __forceinline__ unsigned downwards(unsigned w, unsigned odd) { return odd & (w | nan_codes(w)); }
 
 // A part without keys: its rows' maxima say so, its O stays unwritten.
 template <int ROWS>
@@ -146,7 +154,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
     const float c = p.scale_log2, slack = kSlack / c;
     const int page = p.c.page, sub_k = col >> 2, key_k = col & 3;
     const int* const table = p.c.table + b * p.c.pitch;
-    bool poisoned = false;                                   // NaN codes were met where only some rows see them
+    bool poisoned = false;                                   // NaN or infinities were met where only some rows see them
 
     auto tile_of = [&](int t) __attribute__((always_inline)) { return t < seen.sink_tiles ? t : t - seen.sink_tiles + seen.first; };
     // the pages of this lane's keys in a tile, for K and for V: -1 where there is none
@@ -248,20 +256,30 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
         float scale = __uint_as_float(ve << 23);
         if (at_edge(key0, at_v)) {
             // Keys without a page have zeros: what was loaded for them are page 0's codes and exponent, which may stand for anything.
-            // NaN codes become zero: the probability 0 of a row that does not see them must not meet them.
-            const unsigned some = sees(key0 + 16 * grp, hi_all, lo_all, at_v >= 0), there = at_v >= 0 ? ~0u : 0u;
+            // NaN and infinities become zero: the probability 0 of a row that does not see them must not meet them.
+            const unsigned there = at_v >= 0 ? ~0u : 0u;
             scale = at_v >= 0 ? scale : 1.f;
-            unsigned bad = 0;
+            unsigned any = 0;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     vr[d][j] &= there;
-                    const unsigned nan = nan_codes(vr[d][j]) >> 7;
-                    vr[d][j] &= ~(nan * 0xffu);
-                    bad |= (nan * 0x10204080u >> 28) << (4 * j);                      // bytes 0 ... 3 to bits 0 ... 3
+                    any |= no_numbers(vr[d][j], ve);
                 }
-            poisoned = poisoned || __builtin_amdgcn_ballot_w64((bad & some) != 0) != 0;
+            if (__builtin_amdgcn_ballot_w64(any != 0) != 0) {
+                const unsigned some = sees(key0 + 16 * grp, hi_all, lo_all, at_v >= 0);
+                unsigned bad = 0;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const unsigned odd = no_numbers(vr[d][j], ve) >> 7;
+                        vr[d][j] &= ~(odd * 0xffu);
+                        bad |= (odd * 0x10204080u >> 28) << (4 * j);                  // bytes 0 ... 3 to bits 0 ... 3
+                    }
+                poisoned = poisoned || __builtin_amdgcn_ballot_w64((bad & some) != 0) != 0;
+            }
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -294,31 +312,36 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
         }
     }
     if (poisoned) {
-        // once more through the tiles at an edge: a NaN for every row that sees a NaN code, in that code's column
+        // once more through the tiles at an edge: what the rows that see NaN or an infinity get, in its column
         for (t = t0 + wave; t < t1; t += NW) {
             const int key0 = tile_of(t) * kTile, key = key0 + 16 * grp;
             load_v(t, lookup(key));
             if (!at_edge(key0, at_v)) continue;
             const unsigned visible = sees(key, hi, lo, at_v >= 0);
+            auto ones = [](unsigned bits) __attribute__((always_inline)) { return (bits & 1) * 0x3f80u | (bits >> 8 & 1) * 0x3f800000u; };      // in bf16
             u32x4 see[2];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                see[j / 4][j % 4] = (visible >> (2 * j) & 1) * 0x3f80u | (visible >> (2 * j + 1) & 1) * 0x3f800000u;     // ones in bf16
+            for (int j = 0; j < 8; ++j) see[j / 4][j % 4] = ones((visible >> (2 * j) & 1) | (visible >> (2 * j + 1) & 1) << 8);
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
-                f32x4 hits = {0.f, 0.f, 0.f, 0.f};
+                f32x4 up = {0.f, 0.f, 0.f, 0.f}, down = {0.f, 0.f, 0.f, 0.f};         // how many a row sees
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    u32x4 ind;
+                    u32x4 ind[2];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const unsigned nan = nan_codes(vr[d][2 * u + j / 2]) >> (16 * (j % 2) + 7);
-                        ind[j] = (nan & 1) * 0x3f80u | (nan >> 8 & 1) * 0x3f800000u;
+                        const unsigned w = vr[d][2 * u + j / 2], odd = no_numbers(w, ve);
+                        ind[0][j] = ones(upwards(w, odd) >> (16 * (j % 2) + 7));
+                        ind[1][j] = ones(downwards(w, odd) >> (16 * (j % 2) + 7));
                     }
-                    hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ind), __builtin_bit_cast(bf16x8, see[u]), hits, 0, 0, 0);
+                    up = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ind[0]), __builtin_bit_cast(bf16x8, see[u]), up, 0, 0, 0);
+                    down = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ind[1]), __builtin_bit_cast(bf16x8, see[u]), down, 0, 0, 0);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) oacc[d][e] = hits[e] > 0.f ? NAN : oacc[d][e];
+                for (int e = 0; e < 4; ++e) {
+                    if (up[e] > 0.f) oacc[d][e] += INFINITY;
+                    if (down[e] > 0.f) oacc[d][e] -= INFINITY;
+                }
             }
         }
     }
@@ -402,10 +425,10 @@ __global__ __launch_bounds__(kTileWaves * 64, D == 64 ? 3 : 2) void attn_kv_tile
     constexpr int STAGE = 2 * kTile * D * 2;              // bytes of a K and a V tile
     constexpr int ROWS = kTileWaves * kTileRows;
     __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
-    // by stage, the last tile: whose group of 16 keys has no page; whose V has a NaN, and which (for tiles at an edge only)
-    __shared__ __attribute__((aligned(16))) int s_gone[2][4];
-    __shared__ int s_nan[2];
-    __shared__ __attribute__((aligned(8))) unsigned short s_bits[2][D][4];
+    // by stage and group of 16 keys, the last tile where the group has no page; where its V has NaN or infinities, and which codes go
+    // upwards and downwards (for tiles at an edge only)
+    __shared__ __attribute__((aligned(16))) int s_gone[2][4], s_odd[2][4];
+    __shared__ __attribute__((aligned(8))) unsigned short s_bits[2][2][D][4];
 
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -485,26 +508,35 @@ __global__ __launch_bounds__(kTileWaves * 64, D == 64 ? 3 : 2) void attn_kv_tile
     };
     // What tile t, loaded, needs before it is decoded: zeros where the sequence holds nothing, a note of groups without a page (for
     // which page 0 was loaded: its exponents, which may be any byte, do not count).
-    // At an edge NaN must not meet the probability 0 of a row that does not see it: zeros too, and a note.
+    // At an edge NaN and infinities must not meet the probability 0 of a row that does not see them: zeros too, and a note.
     auto mend = [&](int t) __attribute__((always_inline)) {
-        if (t < whole && !gap) return;
+        if (__builtin_expect(t < whole && !gap, 1)) return;
         const int left = gap ? 0 : seen.n - (tile_of(min(t, t1 - 1)) * kTile + 16 * wave);
+        const unsigned exponent = ve >> (8 * (shifts >> 8)) & 0xff;
+        unsigned any = 0;
 #pragma unroll
-        for (int n = 0; n < NC; ++n) {
-            unsigned bits = 0;
+        for (int n = 0; n < NC; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int bytes = min(max(left - 4 * j, 0), 4);
-                unsigned w = vr[n][j] & (bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1);
-                const unsigned nan = nan_codes(w) >> 7;
-                if (t >= whole) w &= ~(nan * 0xffu);
-                bits |= (nan * 0x10204080u >> 28) << (4 * j);                         // bytes 0 ... 3 to bits 0 ... 3
-                vr[n][j] = w;
+                vr[n][j] &= bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1;
+                any |= no_numbers(vr[n][j], exponent);
             }
-            if (t >= whole) {
-                s_bits[t & 1][v_row + 64 * n][wave] = (unsigned short)bits;
-                if (bits) s_nan[t & 1] = t;
+        if (t >= whole && __builtin_expect(__builtin_amdgcn_ballot_w64(any != 0) != 0, 0)) {
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                unsigned up = 0, down = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned w = vr[n][j], odd = no_numbers(w, exponent);
+                    up |= ((upwards(w, odd) >> 7) * 0x10204080u >> 28) << (4 * j);    // bytes 0 ... 3 to bits 0 ... 3
+                    down |= ((downwards(w, odd) >> 7) * 0x10204080u >> 28) << (4 * j);
+                    vr[n][j] &= ~((odd >> 7) * 0xffu);
+                }
+                s_bits[t & 1][0][v_row + 64 * n][wave] = (unsigned short)up;
+                s_bits[t & 1][1][v_row + 64 * n][wave] = (unsigned short)down;
             }
+            s_odd[t & 1][wave] = t;
         }
         if (gap) {
             s_gone[t & 1][wave] = t;
@@ -613,18 +645,22 @@ __global__ __launch_bounds__(kTileWaves * 64, D == 64 ? 3 : 2) void attn_kv_tile
 #pragma unroll
             for (int i = 0; i < DB; ++i) oacc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[kk][i], p_piece(kk + 2), oacc[i], 0, 0, 0);
     };
-    // a NaN for every row that sees one
-    auto poison = [&](int t, unsigned visible) __attribute__((always_inline)) {
-        for (int d = 0; d < D; ++d) {
-            const u32x2 bits = *(const u32x2*)s_bits[t & 1][d];
-            const unsigned b0 = __builtin_amdgcn_readfirstlane(bits[0]) >> (8 * half), b1 = __builtin_amdgcn_readfirstlane(bits[1]) >> (8 * half);
-            if (__builtin_amdgcn_readfirstlane(bits[0] | bits[1]) == 0) continue;
+    // what the rows that see NaN or an infinity get, in its column
+    auto poison = [&](int t, unsigned visible, unsigned odd) __attribute__((always_inline)) {
+        const unsigned noted0 = (odd & 1) * 0xffffu | (odd >> 1 & 1) * 0xffff0000u, noted1 = (odd >> 2 & 1) * 0xffffu | (odd >> 3) * 0xffff0000u;
+        for (int x = 0; x < 2 * D; ++x) {
+            const int way = x / D, d = x % D;
+            const u32x2 bits = *(const u32x2*)s_bits[t & 1][way][d];
+            const unsigned w0 = __builtin_amdgcn_readfirstlane(bits[0]) & noted0, w1 = __builtin_amdgcn_readfirstlane(bits[1]) & noted1;
+            if ((w0 | w1) == 0) continue;
+            const unsigned b0 = w0 >> (8 * half), b1 = w1 >> (8 * half);
             unsigned mine = visible & ((b0 & 0xff) | (b0 >> 8 & 0xff00) | (b1 & 0xff) << 16 | (b1 >> 8 & 0xff00) << 16);
             mine |= __shfl_xor(mine, 32);
+            const float far = way ? -INFINITY : INFINITY;
 #pragma unroll
             for (int i = 0; i < DB; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) oacc[i][e] = mine != 0 && d == 32 * i + 8 * (e / 4) + 4 * half + e % 4 ? NAN : oacc[i][e];
+                for (int e = 0; e < 16; ++e) oacc[i][e] += mine != 0 && d == 32 * i + 8 * (e / 4) + 4 * half + e % 4 ? far : 0.f;
         }
     };
     // which of the 32 keys of this lane's scores its row sees
@@ -641,19 +677,19 @@ __global__ __launch_bounds__(kTileWaves * 64, D == 64 ? 3 : 2) void attn_kv_tile
     };
 
     if (t0 < t1) {
-        if (tid < 8) { s_nan[tid & 1] = -1; s_gone[tid & 1][tid >> 1] = -1; }
+        if (tid < 8) s_odd[tid & 1][tid >> 1] = s_gone[tid & 1][tid >> 1] = -1;
         find(t0); load(); find(t0 + 1);
         barrier();
         mend(t0); put(t0); load(); find(t0 + 2);
         barrier();
     }
-    auto groups = [&](int t) __attribute__((always_inline)) {                // which groups of 16 keys have a page
-        return ~(unsigned)__builtin_amdgcn_ballot_w64(lane < 4 && s_gone[t & 1][lane & 3] == t) & 15;
+    auto noted = [&](const int (&s)[2][4], int t) __attribute__((always_inline)) {      // for which groups of 16 keys
+        return (unsigned)__builtin_amdgcn_ballot_w64(lane < 4 && s[t & 1][lane & 3] == t);
     };
     int t = t0;
     for (; t < min(t1, whole); ++t) {
         asm volatile("" : "+v"(k_read), "+v"(v_read), "+v"(k_write), "+v"(v_write));     // (offsets are cheaper to make again than to keep)
-        if (groups(t) != 15) break;                                          // a page is missing: the general loop goes on
+        if (noted(s_gone, t) != 0) break;                                        // a page is missing: the general loop goes on
         mend(t + 1);
         scores(t);
         advance(t);
@@ -663,7 +699,7 @@ __global__ __launch_bounds__(kTileWaves * 64, D == 64 ? 3 : 2) void attn_kv_tile
     for (; t < t1; ++t) {
         asm volatile("" : "+v"(k_read), "+v"(v_read), "+v"(k_write), "+v"(v_write));
         const int key0 = tile_of(t) * kTile;
-        const unsigned there = groups(t);
+        const unsigned there = ~noted(s_gone, t) & 15;
         mend(t + 1);
         advance(t);
         // nothing for this wavefront behind its last row's position, or in front of its first row's window
@@ -673,7 +709,8 @@ __global__ __launch_bounds__(kTileWaves * 64, D == 64 ? 3 : 2) void attn_kv_tile
 #pragma unroll
             for (int j = 0; j < 32; ++j) sc[j / 16][j % 16] = visible >> j & 1 ? sc[j / 16][j % 16] : -INFINITY;
             weigh(t);
-            if (__builtin_amdgcn_readfirstlane(s_nan[t & 1]) == t) poison(t, visible);
+            const unsigned odd = noted(s_odd, t);
+            if (__builtin_expect(odd != 0, 0)) poison(t, visible, odd);
         }
         barrier();
     }

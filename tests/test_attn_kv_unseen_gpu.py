@@ -121,3 +121,66 @@ def test_a_cache_as_it_is_allocated():
             o, lse = binding.attn_kv_fp8(bf16_cuda(q), cache, tab, start, q_lens=count, causal=True, wg_rows=wg_rows)
             torch.cuda.synchronize()
             check((host(o), host(lse).astype(np.float64)), want, (S, wg_rows))
+
+
+# (position, column, code): 2^120 times 256 and more is infinite in bf16
+def spoilt_value(cache, table, page, pos, d, code):
+    """V of the page that holds a position at the largest exponent, its other codes small, this code at column d."""
+    at = table[0, pos // page]
+    if cache[3][at, 0] != 247:
+        cache[3][at, 0] = 247
+        cache[1][at, 0] &= 0x07                                 # 2^111 at the most: sums of them are finite
+    cache[1][at, 0, d, pos % page] = code
+
+
+@pytest.mark.parametrize("Sq,D,window", [(4, 128, 0), (4, 64, 30), (70, 128, 0), (200, 64, 40)])
+@pytest.mark.parametrize("wg_rows,splits", [(16, 1), (16, 3), (128, 1), (128, 2)])
+def test_infinite_values_reach_the_rows_that_see_them(Sq, D, window, wg_rows, splits):
+    """Infinities among the last tokens, at a window's end, behind the last token and where every row sees them: the sign's
+    infinity in their column for the rows that see one, NaN for those that see both, the other rows as if they were not there."""
+    rng = np.random.default_rng(Sq + wg_rows + splits)
+    n, page = Sq + 91, 16
+    table, P = make_table(rng, [n], page)
+    clean = make_cache(rng, P, 1, page, D)
+    q = bf16(rng.standard_normal((1, 2, Sq, D)))
+    row_pos = n - Sq + np.arange(Sq)
+    for places in ([(n - 2, 5, 0x78)], [(n - Sq, D - 1, 0xFE)], [(n, 3, 0x7E)], [(70, 9, 0xF8)], [(3, 0, 0x7C)],
+                   [(n - 1, 2, 0x7E), (n - 3, 2, 0xFE)], [(n - 2, 4, 0x7E), (n - 1, 4, 0x7F)]):
+        spoilt, zeroed = [t.copy() for t in clean], [t.copy() for t in clean]
+        up, down, nan = (np.zeros((Sq, D), dtype=bool) for _ in range(3))
+        for pos, d, code in places:
+            spoilt_value(spoilt, table, page, pos, d, code)
+            spoilt_value(zeroed, table, page, pos, d, 0)
+            sees = (pos <= row_pos) & ((pos > row_pos - window) if window else True) & (pos < n)
+            (nan if code == 0x7F else down if code & 0x80 else up)[sees, d] = True
+        nan |= up & down
+        wo, wl, to, tl = attn_reference(q, zeroed, table, [n], None, True, window, 0, D ** -0.5)
+        o, lse = call(q, spoilt, table, [n], window=window, splits=splits, wg_rows=wg_rows)
+        for h in range(2):
+            assert np.array_equal(np.isnan(o[0, h]), nan), places
+            assert np.array_equal(np.isposinf(o[0, h]), up & ~nan) and np.array_equal(np.isneginf(o[0, h]), down & ~nan), places
+            o[0, h][up | down | nan] = wo[0, h][up | down | nan]
+        check((o, lse), (wo, wl, to, tl), places)
+
+
+@pytest.mark.parametrize("Sq", [3, 60])
+def test_the_largest_numbers_written_behind_the_mask(Sq):
+    """A token of +-1.99 * 2^127, which the cache holds as infinities, as the last one: the rows before it do not see it."""
+    import torch
+    from paper_2604_18616_amd import binding
+    rng = np.random.default_rng(Sq)
+    D, page, n = 128, 64, 130
+    table, P = make_table(rng, [n], page)
+    cache, tab = binding.kv_fp8_cache(P, 1, page, D), torch.from_numpy(table).cuda()
+    k, v = (bf16(rng.standard_normal((1, 1, n, D))) for _ in range(2))
+    v[0, 0, -1] = bf16(1.99 * 2.0 ** 127 * np.where(np.arange(D) % 3, 1.0, -1.0))
+    binding.kv_fp8_write(cache, bf16_cuda(k), bf16_cuda(v), tab, whole([0]))
+    q = bf16(rng.standard_normal((1, 4, Sq, D)))
+    torch.cuda.synchronize()
+    held = [host(t) for t in cache]
+    want = attn_reference(q[:, :, :-1], held, table, [n - 1], None, True, 0, 0, D ** -0.5)
+    for wg_rows in (16, 128):
+        for splits in (1, 2):
+            o, lse = call(q, held, table, [n], splits=splits, wg_rows=wg_rows)
+            assert np.isinf(o[0, :, -1]).all() and (np.signbit(o[0, :, -1]) == (np.arange(D) % 3 == 0)).all()
+            check((o[:, :, :-1], lse[:, :, :-1]), want, (wg_rows, splits))
