@@ -574,10 +574,11 @@ def rope_frequencies(R, base=10000.0, factor=1.0, original_len=0, slow=1.0, fast
     """The frequencies of R rotated columns (float64 [R/2], radians per position) as rope_bf16 takes them; factor and
     original_len stretch them for long contexts (include/rope.h)."""
     import torch
-    if int(R) < 2 or int(R) % 2:
+    R, original_len = _int32(int(R), "R"), _int32(int(original_len), "original_len")
+    if R < 2 or R % 2:
         raise ValueError("R must be even and at least 2")
-    values = (ctypes.c_double * (int(R) // 2))()
-    rc = load_library().rope_frequencies(int(R), float(base), float(factor), int(original_len), float(slow), float(fast), values)
+    values = (ctypes.c_double * (R // 2))()
+    rc = load_library().rope_frequencies(R, float(base), float(factor), original_len, float(slow), float(fast), values)
     if rc != 0:
         raise AttnError(rc, strerror(rc))
     return torch.tensor(list(values), dtype=torch.float64, device=device)
@@ -615,10 +616,11 @@ def rope_bf16(q, positions, inv_freq, k=None, q_out=None, k_out=None, interleave
         raise ValueError("positions must be int32 [B, S] or [S] with contiguous rows on q's device")
     if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous() or inv_freq.device != device:
         raise ValueError("inv_freq must be a contiguous float64 vector on q's device")
+    R = _int32(2 * inv_freq.numel(), "twice the number of frequencies")
     stream, _ = _streams(q, stream)
     with _on(device):
         rc = load_library().rope_bf16(q.data_ptr(), q_out.data_ptr(), k.data_ptr() if Hk else None, k_out.data_ptr() if Hk else None, B, Hq, Hk, S, D,
-                                      2 * inv_freq.numel(), qs, qos, ks, kos, positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0,
+                                      R, qs, qos, ks, kos, positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0,
                                       inv_freq.data_ptr(), 1 if interleaved else 0, 1 if inverse else 0, float(scale), stream)
     if rc != 0:
         raise AttnError(rc, strerror(rc))
