@@ -541,7 +541,7 @@ def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=Fal
     import torch
     struct, H, D, device = _cache_struct(cache)
     at, pitch, B, width = _table(table, device)
-    if q.dim() != 4 or q.shape[1] % H:
+    if q.dim() != 4 or H < 1 or q.shape[1] % H:
         raise ValueError("q must be [B, Hq, Sq, D] with Hq a multiple of the cache's heads")
     Hq, Sq = q.shape[1], q.shape[2]
     shape = (B, Hq, Sq, D)
@@ -552,7 +552,7 @@ def attn_kv_fp8(q, cache, table, lens, q_lens=None, o=None, lse=None, causal=Fal
         lse = torch.empty((B, Hq, Sq), dtype=torch.float32, device=device)
     elif lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, Sq) or not lse.is_contiguous() or lse.device != device:
         raise ValueError("lse must be a contiguous float32 tensor of shape [B, Hq, Sq] on q's device")
-    scale = float(D) ** -0.5 if scale is None else float(scale)
+    scale = max(D, 1) ** -0.5 if scale is None else float(scale)            # (D = 0 is the library's to refuse)
     window, sinks, max_len, wg_rows = (_int32(n, name) for n, name in ((window, "window"), (sinks, "sinks"), (max_len, "max_len"), (wg_rows, "wg_rows")))
     lens, q_lens = _per_sequence(lens, B, device, "lens"), _per_sequence(q_lens, B, device, "q_lens")
     stream, own = _streams(q, stream)
