@@ -390,7 +390,8 @@ class _CacheStruct(ctypes.Structure):
 
 def kv_fp8_cache(pages, Hkv, page, D, device="cuda") -> KvFp8Cache:
     """An empty cache of `pages` pages of `page` tokens (16, 32, 64 or 128) for Hkv kv heads of dimension D (64 or 128); its
-    contents mean nothing before they are written."""
+    contents mean nothing before they are written, and no call heeds those of pages that no sequence holds.  Small pages make the
+    write of a single token cheaper (include/kv_cache.h), large ones the table shorter."""
     import torch
     codes = lambda *shape: torch.empty(shape, dtype=torch.uint8, device=device)
     return KvFp8Cache(codes(pages, Hkv, page, D), codes(pages, Hkv, D, page), codes(pages, Hkv), codes(pages, Hkv))

@@ -15,7 +15,7 @@
 // the workgroups of a row by attn_kv_join or attn_kv_combine from fp32 parts.
 // What bounds it: reading the codes, or latency.  32 sequences of up to 8191 keys, 8 kv heads of 128: 63 us = 4.4 TB/s; 16 of up to
 // 20000 keys with a window of 4096, 16 heads of 64: 25 us = 5.0 TB/s (a copy reaches 4.9); one of 131071 keys, one kv head: 13.6 us
-// (10 and 3.5 in the two kernels); one of 2000 keys, 8 kv heads: 10 us (6 and 4).  Many rows have a kernel of their own below.
+// (10 and 3.5 in the two kernels); one of 2000 keys, 8 kv heads: 9.5 us (5.5 and 4).  Many rows have a kernel of their own below.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <math.h>
@@ -402,8 +402,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_kv_rows(KvAttnParams p) {
 // Row m of a 32-key block of S^T stands for key m with bits 2 and 3 exchanged: then the eight scores that a lane holds for a
 // step of 16 keys are those of eight consecutive keys, one 16-byte piece of its row of V^T.
 //
-// What bounds it: 2 x 1000 rows of 32 heads of 128 against up to 16301 keys take 380 us, 1010 TFLOP/s (a large matrix product
-// 1366); the matrix units are busy 50 % of that, the vector units 51 %, LDS 38 %: the wavefronts' turns at them overlap in part.
+// What bounds it: 2 x 1000 rows of 32 heads of 128 against up to 16301 keys take 390 to 402 us, 955 to 985 TFLOP/s (a large matrix
+// product 1366); the matrix units are busy 49 % of that, the vector units 50 %, LDS 37 %: the wavefronts' turns at them overlap in part.
 // Two workgroups on a CU (three for D = 64, which its 169 registers just miss without being asked: 4 x 1500 rows against 8000 keys
 // 238 -> 183 us) measured better than one of eight wavefronts; codes kept as they are in LDS and decoded at every read 554 us;
 // a wavefront's priority raised around its matrix instructions 408 to 422; the first 32 keys' probabilities made while the other 32
@@ -856,7 +856,7 @@ __global__ __launch_bounds__(256) void attn_kv_join(KvAttnParams p) {
 // times that where both are alike.  Parts cost a second kernel and their traffic.
 static double estimate(const KvAttnPlan& plan, long long pairs, long long rows, int tiles, int D) {
     const bool rows16 = plan.rows == kBlock, wide = D == 128, single = plan.waves == 1;
-    const long long n = pairs * plan.row_wgs * plan.splits, slots = rows16 && plan.waves == 8 ? 256 : (wide ? 2048 : 3072) / plan.waves;
+    const long long n = pairs * plan.row_wgs * plan.splits, slots = rows16 && plan.waves == 8 ? 256 : 256 * (wide ? 8 : 12) / plan.waves;      // on 256 CUs
     const double start = single ? 4.6 : rows16 ? (plan.waves == 8 ? (wide ? 6.6 : 5.6) : wide ? 5.2 : 4.8) : 6.5;
     // a step is a tile of every wavefront (rows) or of the workgroup: with one wavefront on a SIMD, with two, and with the CU full
     const double alone = single ? (wide ? 0.95 : 0.6) : rows16 ? (plan.waves == 8 ? (wide ? 2.5 : 1.0) : wide ? 1.3 : 0.72) : wide ? 1.21 : 0.95;
@@ -881,7 +881,7 @@ static double estimate(const KvAttnPlan& plan, long long pairs, long long rows, 
 // How many rows a workgroup takes, by how many wavefronts, and how the keys are cut: whatever is estimated to be the fastest.
 // Measured, rows of 16 / of 128 per workgroup, sequences x keys, D = 128, 8 kv heads: 32 packed rows 1 x 64000 35.5 / 47.0 us,
 // 64 x 1000 39.5 / 45.0; 64 rows 55.9 / 50.2, 61.1 / 46.6; 128 rows 96.6 / 57.4, but 1 x 1000 11.6 / 16.2.  A wavefront by itself
-// or four, sequences x keys, 8 kv heads of 128: 256 x 60 11.1 / 22.4 us, 256 x 250 30.2 / 36.5, but 16 x 250 8.4 / 6.4; where several
+// or four, sequences x keys, 8 kv heads of 128: 256 x 60 10.4 / 22.4 us, 256 x 250 30.2 / 36.5, but 16 x 250 8.4 / 6.4; where several
 // row blocks share keys that are cut it is slower than estimated (2 blocks, 1 x 3781 14.0 / 11.2), and left out.
 KvAttnPlan attn_kv_plan(int B, int Hq, int Hkv, int Sq, int keys, int D, int splits, int wg_rows) {
     static const int kCuts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};

@@ -67,7 +67,7 @@ __device__ __forceinline__ unsigned largest(u32x4 w, unsigned m) {
 // FEW: at most kFewTokens new tokens lie in few blocks and two pieces, for which a wavefront does on larger pages too: one token of
 // 99 sequences and 16 heads, pages of 64, 15.8 -> 11.3 us, 16 of 16 sequences and 8 heads, pages of 128, 8.4 -> 7.1 (17 tokens, by 256
 // threads, 8.6).  One token of 64 sequences, 8 heads, pages of 16 / 64 / 128: 5.3 / 6.9 / 7.4 us in a captured graph (every column's
-// byte of V lies in another line); 7.4 / 11.9 / 15.6 between two events where scales grow, 7.0 / 8.8 / 9.4 where they do not.
+// byte of V lies in another line); 7.4 / 12.0 / 15.8 between two events where scales grow, 7.0 / 8.7 / 9.4 where they do not.
 constexpr int kFewTokens = 16;
 template <int D, int PAGE, bool FEW>
 __global__ __launch_bounds__(kThreads) void kv_write(KvWriteParams p) {
@@ -222,6 +222,7 @@ __device__ __forceinline__ void decode16(u32x4 c, float scale, unsigned (&out)[8
 // 64 positions of one sequence and kv head, keys (blockIdx.y 0) or values.  Keys go straight through; a thread with values holds
 // 16 tokens of two columns, which meet their rows in LDS (dword c of the rows of group g lies at c ^ 16 g: no bank conflicts).
 // 8 sequences of up to 4001 positions, 8 heads of 128: 34.5 us a call = 4.9 TB/s (25 in the kernel while the codes are still cached).
+// From a position inside a group of 16 on, V goes code by code: 44 us in place of 26 in a captured graph.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv_read(KvReadParams p) {
     constexpr int CPR = D / 16, NK = kReadRows * CPR / kThreads;
