@@ -17,7 +17,8 @@
  *
  * What the page size costs: larger pages need fewer exponents and table entries, smaller ones make a single token's write cheaper,
  * since every column's code of V lies in another line and a scale that grows has the page rounded again.  One token of 64 sequences
- * and 8 heads of 128, pages of 16 / 32 / 64 / 128: 7.0 / 8.4 / 8.7 / 9.4 us, and 7.4 / 9.8 / 12.0 / 15.8 where every scale grows.
+ * and 8 heads of 128, pages of 16 / 32 / 64 / 128: 7.0 / 8.4 / 8.7 / 9.4 us, and 7.4 / 9.8 / 12.0 / 15.8 where every scale
+ * grows (between two events).
  *
  * All pointers except the strides and the KvFp8Cache itself are DEVICE pointers into caller-owned memory.  The library
  * neither allocates nor frees nor synchronises: every call enqueues its kernels on `stream` (a hipStream_t as void*, NULL =
